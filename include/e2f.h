@@ -343,6 +343,130 @@ e2f_status e2f_eaas_tensor_product(e2f_ctx *ctx, const void *h, const float *r, 
                                    int32_t T, void *hip_stream);
 
 /*
+ * The all-pair block: what a model runs on invariant features of the atoms beside the cutoff attention (not part of the
+ * paper's operator, which it leaves as it is).  Its operands are rows of heads, element (token t, head h, feature d) at
+ * ptr[t * token_stride + h * head_stride + d]; the strides count elements.
+ *   ptr           device, 16-byte aligned
+ *   token_stride, head_stride  >= 0 and multiples of 16 bytes: E2F_ERR_UNSUPPORTED otherwise.  A stride of 0 repeats a
+ *                 row and is for operands that are read; rows of a result must not overlap (E2F_ERR_INVALID_ARG).
+ * None of these calls allocates or synchronises, so all of them can be captured into a graph; a graph keeps the
+ * workspace that it was captured with, and two calls that overlap in time need a workspace each.  The device that
+ * hip_stream belongs to must be the current device.  Results do not depend on the order in which workgroups run.
+ */
+typedef struct {
+    void *ptr;
+    int64_t token_stride, head_stride;
+} e2f_heads;
+
+/*
+ * Norms of queries and keys for each head with the rotation by the position along a chain (the index of a residue or
+ * monomer, which no rotation or translation of the atoms changes) in the same pass.  For each token t and head, with x
+ * a row of D features and w the weight of its kind:
+ *   u_d = w_d x_d (mean_d x_d^2 + eps)^(-1/2)
+ *   y   = u with the first rotary_dim features turned pairwise: for pair i of rotary_dim/2, features a and b,
+ *         y_a = u_a cos f - u_b sin f,  y_b = u_b cos f + u_a sin f,  f = position[t] position_scale theta^(-2i/rotary_dim)
+ *         HALF: (a, b) = (i, i + rotary_dim/2);  INTERLEAVED: (2i, 2i + 1)
+ * Angles are formed in 64 bits and reduced to one turn before they are rounded; everything else is binary32, rounded
+ * once to the feature type.  q and q_out (k and k_out) may be the same rows; other overlaps are not allowed.
+ * Hq or Hk may be 0 (its e2f_heads is then ignored and may be NULL), for queries and keys of different tokens.
+ */
+typedef enum { E2F_ROTARY_HALF = 0, E2F_ROTARY_INTERLEAVED = 1 } e2f_rotary_layout;
+typedef struct {
+    int32_t dtype;          /* e2f_dtype of q, k and the gradients of both */
+    int32_t N, Hq, Hk;      /* tokens; heads of q and of k, each 0..1024 */
+    int32_t D;              /* features of a head, a multiple of 8, 8..256 */
+    int32_t rotary_dim;     /* even, 0 (no rotation) .. D */
+    int32_t layout;         /* e2f_rotary_layout */
+    float eps;              /* > 0 */
+    double theta;           /* > 0 */
+    double position_scale;  /* finite; below 1 it compresses the positions of chains longer than a model was trained on */
+    const int32_t *position;                  /* device [N]; may be NULL if rotary_dim is 0 */
+    const float *weight_q, *weight_k;         /* device [D]; NULL: ones */
+} e2f_qk_args;
+e2f_status e2f_qk_norm_rotate(const e2f_qk_args *a, const e2f_heads *q, const e2f_heads *k, const e2f_heads *q_out,
+                              const e2f_heads *k_out, void *hip_stream);
+/*
+ * Its backward pass, from q, k (before the norm) and the gradients of its results.
+ *   grad_q, grad_k              dL/dq, dL/dk; may be the same rows as grad_q_out, grad_k_out
+ *   grad_weight_q, grad_weight_k  device float [D], sums over tokens and heads, fully overwritten; NULL: not wanted
+ *   ws   device, at least e2f_qk_norm_rotate_backward_workspace_bytes(a) bytes, 256-byte aligned
+ */
+size_t e2f_qk_norm_rotate_backward_workspace_bytes(const e2f_qk_args *a);
+e2f_status e2f_qk_norm_rotate_backward(const e2f_qk_args *a, const e2f_heads *q, const e2f_heads *k,
+                                       const e2f_heads *grad_q_out, const e2f_heads *grad_k_out, const e2f_heads *grad_q,
+                                       const e2f_heads *grad_k, float *grad_weight_q, float *grad_weight_k, void *ws,
+                                       size_t ws_bytes, void *hip_stream);
+
+/*
+ * Attention among all atoms of a segment, whatever their distance.  For query i and key j of the same segment, query
+ * head h and its key head h' = h / (Hq/Hk):
+ *   x_ij = scale q_i,h . k_j,h'
+ *   s_ij = cap tanh(x_ij / cap) - slope_h |r_i - r_j|        (cap = 0: x_ij itself; no slope: without the second term)
+ *   out_i,h = sum_j softmax_j(s_ij) v_j,h'
+ * j = i is included where queries and keys are the same atoms.  The radial basis of the cutoff attention ends at the
+ * cutoff; the bias here goes on, falling with the distance at a rate that each head learns (a slope may be negative).
+ * Queries and keys may also be different tokens, a readout token or a probe over a whole system for one: with few
+ * queries the keys are split over workgroups and the parts joined.
+ *   q_offsets, k_offsets  device int32 [S+1], non-decreasing from 0 (not checked on the host; a segment is cut to the
+ *                 tokens there are): segment s has the queries [q_offsets[s], q_offsets[s+1]), the keys likewise
+ *   q_lengths, k_lengths  device int32 [S] or NULL: only the first tokens of each segment count (a padded batch); values
+ *                 are cut to 0 .. the segment's size
+ *   q_pos, k_pos, slope   device float [Nq][3], [Nk][3], [Hq]; all three or none
+ * Keys outside their segment's length and queries outside any segment's are not read.  A query without keys gets a zero row;
+ * rows of out and of the gradients that no segment's length covers are left as they were.
+ * Scores, softmax statistics and sums are binary32; with bf16 features the weights of the sum over v and the two factors of
+ * the gradients' sums are rounded to bf16 for the matrix cores.
+ */
+typedef struct {
+    int32_t dtype;          /* e2f_dtype of q, k, v, out and their gradients */
+    int32_t Hq, Hk;         /* query and key heads, Hq a multiple of Hk, 1..1024 */
+    int32_t D;              /* features of a head, a multiple of 8, 8..128 */
+    int32_t Nq, Nk, S;      /* query tokens, key tokens, segments */
+    float scale;            /* finite */
+    float cap;              /* > 0, or 0 for none */
+    const int32_t *q_offsets, *k_offsets, *q_lengths, *k_lengths;
+    const float *q_pos, *k_pos, *slope;
+} e2f_dense_args;
+/*
+ * ws: device, at least e2f_dense_attn_workspace_bytes(a) bytes (may be 0: ws may then be NULL), 256-byte aligned.  Both workspace
+ * queries go by the sizes alone and follow no pointer; the backward pass's asks for more if slope is not NULL.
+ */
+size_t e2f_dense_attn_workspace_bytes(const e2f_dense_args *a);
+e2f_status e2f_dense_attn_forward(const e2f_dense_args *a, const e2f_heads *q, const e2f_heads *k, const e2f_heads *v,
+                                  const e2f_heads *out, void *ws, size_t ws_bytes, void *hip_stream);
+/*
+ * Its backward pass from the same operands and dL/dout; the softmax statistics are formed again in binary32, so that it
+ * needs nothing of the forward call.
+ *   grad_q, grad_k, grad_v   rows of the feature type; gradients of a key head are summed over the query heads that share it
+ *   grad_slope               device float [Hq], fully overwritten, or NULL
+ *   grad_q_pos, grad_k_pos   device float [Nq][3], [Nk][3] or NULL: what q_pos and k_pos get as the queries' and as the keys'
+ *                 places (add the two where they are the same atoms).  The distance of an atom to itself has gradient 0.
+ * The last three need slope (E2F_ERR_INVALID_ARG).
+ */
+size_t e2f_dense_attn_backward_workspace_bytes(const e2f_dense_args *a);
+e2f_status e2f_dense_attn_backward(const e2f_dense_args *a, const e2f_heads *q, const e2f_heads *k, const e2f_heads *v,
+                                   const e2f_heads *grad_out, const e2f_heads *grad_q, const e2f_heads *grad_k,
+                                   const e2f_heads *grad_v, float *grad_slope, float *grad_q_pos, float *grad_k_pos,
+                                   void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Global norm of a training step's gradients (those of e2f_attn_backward's weights, for instance) and clipping by it:
+ *   norm = (sum over all elements of all tensors of g^2)^(1/2),  out = g * min(1, max_norm / (norm + 1e-6))
+ * Squares and sums are binary64, so no finite gradient overflows.  If norm is not finite, out = g: the caller sees it in
+ * *norm and skips the step.
+ *   n                 tensors, >= 0
+ *   grads, out        host arrays [n] of device pointers, contiguous tensors; out[i] may be grads[i], any other overlap is
+ *                     not allowed.  Tensors may start at any element.
+ *   counts, dtypes    host arrays [n]: elements (>= 0) and e2f_dtype of each.  All four arrays are read before the call returns.
+ *   max_norm          > 0 (infinity: the norm alone, out = g)
+ *   norm              device float [1]
+ *   ws                device, at least e2f_grad_norm_clip_workspace_bytes(n, counts) bytes, 256-byte aligned
+ */
+size_t e2f_grad_norm_clip_workspace_bytes(int32_t n, const int64_t *counts);
+e2f_status e2f_grad_norm_clip(int32_t n, void *const *grads, void *const *out, const int64_t *counts, const int32_t *dtypes,
+                              float max_norm, float *norm, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
  * Per-stage timing of e2f_attn_forward for benchmarks (measurement aid; callers that do not ask for it pay
  * nothing).  e2f_profile_begin creates HIP events for up to max_calls calls; while profiling is on, every
  * e2f_attn_forward records events between its stages on the stream it is given (no synchronisation).

@@ -12,7 +12,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "csrc", "libe2f.so")
 
-E2F_OK = 0
+E2F_OK, E2F_ERR_INVALID_ARG = 0, 1
 E2F_F32, E2F_BF16 = 0, 1
 ATTENTION = {"auto": 0, "tile": 1, "pair": 2, "valu": 3}   # e2f_attn_kernel
 E2F_FLAG_TILE_LISTS_PER_HEAD, E2F_FLAG_PROJECT_PER_CHANNEL_TILE = 1, 2
@@ -26,7 +26,10 @@ EXPORTS = ["e2f_status_string", "e2f_create", "e2f_destroy", "e2f_cells_workspac
            "e2f_attn_backward_workspace_bytes", "e2f_attn_backward", "e2f_attn_backward_after_forward",
            "e2f_attn_backward_weights_workspace_bytes", "e2f_attn_nonlinear_workspace_bytes",
            "e2f_attn_forward_nonlinear", "e2f_count_edges", "e2f_profile_read",
-           "e2f_attn_forward_static"]
+           "e2f_attn_forward_static", "e2f_qk_norm_rotate", "e2f_qk_norm_rotate_backward_workspace_bytes",
+           "e2f_qk_norm_rotate_backward", "e2f_dense_attn_workspace_bytes", "e2f_dense_attn_forward",
+           "e2f_dense_attn_backward_workspace_bytes", "e2f_dense_attn_backward", "e2f_grad_norm_clip_workspace_bytes",
+           "e2f_grad_norm_clip"]
 STATIC_SCRATCH_BYTES = 32 << 20   # E2F_STATIC_SCRATCH_BYTES
 STAGES = ("prepare", "project", "attention")
 
@@ -39,6 +42,24 @@ class Config(ctypes.Structure):
 
 class Weights(ctypes.Structure):
     _fields_ = [(k, ctypes.c_void_p) for k in ("WQ1", "WQ2", "WK1", "WK2", "WV", "Wb", "w_path")]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class QkArgs(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("N", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hk", ctypes.c_int32),
+                ("D", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("theta", ctypes.c_double), ("position_scale", ctypes.c_double), ("position", ctypes.c_void_p),
+                ("weight_q", ctypes.c_void_p), ("weight_k", ctypes.c_void_p)]
+
+
+class DenseArgs(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hk", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("Nq", ctypes.c_int32), ("Nk", ctypes.c_int32), ("S", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("cap", ctypes.c_float)] + [(n, ctypes.c_void_p) for n in (
+                    "q_offsets", "k_offsets", "q_lengths", "k_lengths", "q_pos", "k_pos", "slope")]
 
 
 class E2fError(RuntimeError):
@@ -123,6 +144,25 @@ def load():
     L.e2f_profile_begin.restype = ctypes.c_int
     L.e2f_profile_end.argtypes = [vp, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(i32)]
     L.e2f_profile_end.restype = ctypes.c_int
+    heads, qk, dense = ctypes.POINTER(Heads), ctypes.POINTER(QkArgs), ctypes.POINTER(DenseArgs)
+    L.e2f_qk_norm_rotate.argtypes = [qk, heads, heads, heads, heads, vp]
+    L.e2f_qk_norm_rotate.restype = ctypes.c_int
+    L.e2f_qk_norm_rotate_backward_workspace_bytes.argtypes = [qk]
+    L.e2f_qk_norm_rotate_backward_workspace_bytes.restype = sz
+    L.e2f_qk_norm_rotate_backward.argtypes = [qk] + [heads] * 6 + [vp, vp, vp, sz, vp]
+    L.e2f_qk_norm_rotate_backward.restype = ctypes.c_int
+    L.e2f_dense_attn_workspace_bytes.argtypes = [dense]
+    L.e2f_dense_attn_workspace_bytes.restype = sz
+    L.e2f_dense_attn_forward.argtypes = [dense] + [heads] * 4 + [vp, sz, vp]
+    L.e2f_dense_attn_forward.restype = ctypes.c_int
+    L.e2f_dense_attn_backward_workspace_bytes.argtypes = [dense]
+    L.e2f_dense_attn_backward_workspace_bytes.restype = sz
+    L.e2f_dense_attn_backward.argtypes = [dense] + [heads] * 7 + [vp, vp, vp, vp, sz, vp]
+    L.e2f_dense_attn_backward.restype = ctypes.c_int
+    L.e2f_grad_norm_clip_workspace_bytes.argtypes = [i32, vp]
+    L.e2f_grad_norm_clip_workspace_bytes.restype = sz
+    L.e2f_grad_norm_clip.argtypes = [i32, vp, vp, vp, vp, ctypes.c_float, vp, vp, sz, vp]
+    L.e2f_grad_norm_clip.restype = ctypes.c_int
     _lib = L
     return L
 
@@ -323,6 +363,181 @@ def e2f_eaas_tensor_product(ctx, h, r, w_path, out):
     """h [T][n][C] (feature dtype), r float32 [T][3], w_path float32 [L+1][L+1], out float32 [T][n][C]."""
     _check(load().e2f_eaas_tensor_product(ctx, _ptr(h), _ptr(r), _ptr(w_path), _ptr(out), h.shape[0], _stream()),
            "e2f_eaas_tensor_product")
+
+
+# ---- the all-pair block -------------------------------------------------------------------------------------------
+# These calls run on the device of their tensors, on its current stream, and check shapes, types and devices: the C call
+# sees pointers alone.  A refused tensor raises E2fError with E2F_ERR_INVALID_ARG; `where` names the call and the tensor.
+
+ROTARY = {"half": 0, "interleaved": 1}
+
+
+def _need(ok, where):
+    if not ok:
+        raise E2fError(E2F_ERR_INVALID_ARG, where)
+
+
+def _feature_type(t, where):
+    import torch
+    _need(t.dtype in (torch.float32, torch.bfloat16), where)
+    return E2F_BF16 if t.dtype == torch.bfloat16 else E2F_F32
+
+
+def _heads(t, like, shape, where):
+    """[N][H][D] tensor of the type and on the device of `like`, features side by side -> Heads."""
+    _need(t.dtype == like.dtype and t.device == like.device and t.shape == shape and (shape[2] <= 1 or t.stride(2) == 1), where)
+    s = t.stride()
+    return Heads(t.data_ptr(), s[0], s[1])
+
+
+def _plain(t, like, dtype, shape, where):
+    """Contiguous tensor of a type and shape on the device of `like` -> its address; None -> None."""
+    if t is None:
+        return None
+    _need(t.dtype == dtype and t.device == like.device and t.shape == shape and t.is_contiguous(), where)
+    return t.data_ptr()
+
+
+def _on(device, call, *args):
+    """call(*args, stream) with the device current."""
+    import torch
+    _need(device.type == "cuda", call.__name__)
+    if device.index == torch.cuda.current_device():
+        return call(*args, torch.cuda.current_stream(device).cuda_stream)
+    with torch.cuda.device(device):
+        return call(*args, torch.cuda.current_stream(device).cuda_stream)
+
+
+def _bytes_of(ws, like, where):
+    import torch
+    _need(ws is None or (ws.dtype == torch.uint8 and ws.device == like.device and ws.is_contiguous()), where)
+    return (ws.data_ptr(), ws.numel()) if ws is not None else (None, 0)
+
+
+def _qk_args(where, q, k, position, weight_q, weight_k, rotary_dim, layout, theta, position_scale, eps):
+    import torch
+    _need(q is not None or k is not None, where)
+    x = q if q is not None else k
+    _need(x.dim() == 3, where)
+    N, D = x.shape[0], x.shape[2]
+    a = QkArgs(_feature_type(x, where), N, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], D, rotary_dim,
+               ROTARY.get(layout, layout), eps, theta, position_scale,
+               _plain(position, x, torch.int32, (N,), where + ": position"),
+               _plain(weight_q, x, torch.float32, (D,), where + ": weight_q"),
+               _plain(weight_k, x, torch.float32, (D,), where + ": weight_k"))
+    return a, x, (N, a.Hq, D), (N, a.Hk, D)
+
+
+def _optional_heads(t, like, shape, where):
+    if shape[1] == 0:
+        return Heads()
+    _need(t is not None, where)
+    return _heads(t, like, shape, where)
+
+
+def e2f_qk_norm_rotate(q, k, q_out, k_out, position=None, weight_q=None, weight_k=None, rotary_dim=0, layout="half",
+                       theta=10000.0, position_scale=1.0, eps=1e-6):
+    """q [N][Hq][D], k [N][Hk][D] (either may be None), q_out, k_out alike; position int32 [N]; weights float32 [D]."""
+    where = "e2f_qk_norm_rotate"
+    a, x, sq, sk = _qk_args(where, q, k, position, weight_q, weight_k, rotary_dim, layout, theta, position_scale, eps)
+    rows = [_optional_heads(t, x, s, where + ": " + n)
+            for t, s, n in ((q, sq, "q"), (k, sk, "k"), (q_out, sq, "q_out"), (k_out, sk, "k_out"))]
+    _check(_on(x.device, load().e2f_qk_norm_rotate, a, *rows), where)
+
+
+def e2f_qk_norm_rotate_backward_workspace_bytes(q, k):
+    a = _qk_args("e2f_qk_norm_rotate_backward_workspace_bytes", q, k, None, None, None, 0, 0, 1.0, 1.0, 1.0)[0]
+    return load().e2f_qk_norm_rotate_backward_workspace_bytes(a)
+
+
+def e2f_qk_norm_rotate_backward(q, k, grad_q_out, grad_k_out, grad_q, grad_k, grad_weight_q, grad_weight_k, ws, position=None,
+                                weight_q=None, weight_k=None, rotary_dim=0, layout="half", theta=10000.0, position_scale=1.0,
+                                eps=1e-6):
+    """grad_weight_q, grad_weight_k float32 [D] or None; ws uint8."""
+    import torch
+    where = "e2f_qk_norm_rotate_backward"
+    a, x, sq, sk = _qk_args(where, q, k, position, weight_q, weight_k, rotary_dim, layout, theta, position_scale, eps)
+    rows = [_optional_heads(t, x, s, where + ": " + n)
+            for t, s, n in ((q, sq, "q"), (k, sk, "k"), (grad_q_out, sq, "grad_q_out"), (grad_k_out, sk, "grad_k_out"),
+                            (grad_q, sq, "grad_q"), (grad_k, sk, "grad_k"))]
+    sums = [_plain(t, x, torch.float32, (a.D,), where + ": grad_weight") for t in (grad_weight_q, grad_weight_k)]
+    _check(_on(x.device, load().e2f_qk_norm_rotate_backward, a, *rows, *sums, *_bytes_of(ws, x, where + ": ws")), where)
+
+
+def _dense_args(where, q, k, S, q_offsets=None, k_offsets=None, scale=None, cap=0.0, q_pos=None, k_pos=None, slope=None,
+                q_lengths=None, k_lengths=None):
+    import torch
+    _need(q.dim() == 3 and k.dim() == 3, where)
+    (Nq, Hq, D), (Nk, Hk, _) = q.shape, k.shape
+    ints = [_plain(t, q, torch.int32, (n,), where + ": " + name)
+            for t, n, name in ((q_offsets, S + 1, "q_offsets"), (k_offsets, S + 1, "k_offsets"),
+                               (q_lengths, S, "q_lengths"), (k_lengths, S, "k_lengths"))]
+    floats = [_plain(t, q, torch.float32, shape, where + ": " + name)
+              for t, shape, name in ((q_pos, (Nq, 3), "q_pos"), (k_pos, (Nk, 3), "k_pos"), (slope, (Hq,), "slope"))]
+    return DenseArgs(_feature_type(q, where), Hq, Hk, D, Nq, Nk, S, D ** -0.5 if scale is None else scale, cap, *ints, *floats)
+
+
+def e2f_dense_attn_workspace_bytes(q, k, S):
+    """S segments."""
+    return load().e2f_dense_attn_workspace_bytes(_dense_args("e2f_dense_attn_workspace_bytes", q, k, S))
+
+
+def e2f_dense_attn_forward(q, k, v, q_offsets, k_offsets, out, ws, scale=None, cap=0.0, q_pos=None, k_pos=None, slope=None,
+                           q_lengths=None, k_lengths=None):
+    """q, out [Nq][Hq][D]; k, v [Nk][Hk][D]; q_offsets, k_offsets int32 [S+1]; q_lengths, k_lengths int32 [S] or None;
+    q_pos, k_pos float32 [Nq][3], [Nk][3] and slope float32 [Hq], or None; scale: 1/sqrt(D) unless given; ws uint8."""
+    where = "e2f_dense_attn_forward"
+    a = _dense_args(where, q, k, q_offsets.shape[0] - 1, q_offsets, k_offsets, scale, cap, q_pos, k_pos, slope, q_lengths, k_lengths)
+    sq, sk = (a.Nq, a.Hq, a.D), (a.Nk, a.Hk, a.D)
+    rows = [_heads(t, q, s, where + ": " + n) for t, s, n in ((q, sq, "q"), (k, sk, "k"), (v, sk, "v"), (out, sq, "out"))]
+    _check(_on(q.device, load().e2f_dense_attn_forward, a, *rows, *_bytes_of(ws, q, where + ": ws")), where)
+
+
+def e2f_dense_attn_backward_workspace_bytes(q, k, S):
+    """S segments; the size that serves a call with or without slope."""
+    a = _dense_args("e2f_dense_attn_backward_workspace_bytes", q, k, S)
+    a.slope = 4096      # not followed: whether there is one counts
+    return load().e2f_dense_attn_backward_workspace_bytes(a)
+
+
+def e2f_dense_attn_backward(q, k, v, q_offsets, k_offsets, grad_out, grad_q, grad_k, grad_v, ws, scale=None, cap=0.0, q_pos=None,
+                            k_pos=None, slope=None, q_lengths=None, k_lengths=None, grad_slope=None, grad_q_pos=None,
+                            grad_k_pos=None):
+    """As e2f_dense_attn_forward; grad_slope float32 [Hq], grad_q_pos [Nq][3], grad_k_pos [Nk][3] or None."""
+    import torch
+    where = "e2f_dense_attn_backward"
+    a = _dense_args(where, q, k, q_offsets.shape[0] - 1, q_offsets, k_offsets, scale, cap, q_pos, k_pos, slope, q_lengths, k_lengths)
+    sq, sk = (a.Nq, a.Hq, a.D), (a.Nk, a.Hk, a.D)
+    rows = [_heads(t, q, s, where + ": " + n)
+            for t, s, n in ((q, sq, "q"), (k, sk, "k"), (v, sk, "v"), (grad_out, sq, "grad_out"), (grad_q, sq, "grad_q"),
+                            (grad_k, sk, "grad_k"), (grad_v, sk, "grad_v"))]
+    sums = [_plain(t, q, torch.float32, s, where + ": " + n)
+            for t, s, n in ((grad_slope, (a.Hq,), "grad_slope"), (grad_q_pos, (a.Nq, 3), "grad_q_pos"),
+                            (grad_k_pos, (a.Nk, 3), "grad_k_pos"))]
+    _check(_on(q.device, load().e2f_dense_attn_backward, a, *rows, *sums, *_bytes_of(ws, q, where + ": ws")), where)
+
+
+def e2f_grad_norm_clip_workspace_bytes(grads):
+    n = len(grads)
+    return load().e2f_grad_norm_clip_workspace_bytes(n, (ctypes.c_int64 * n)(*[g.numel() for g in grads]))
+
+
+def e2f_grad_norm_clip(grads, out, max_norm, norm, ws):
+    """grads, out: lists of contiguous float32 or bfloat16 tensors (out may be grads); norm float32 [1]; ws uint8."""
+    import torch
+    where = "e2f_grad_norm_clip"
+    n = len(grads)
+    _need(len(out) == n, where + ": out")
+    _need(norm.dtype == torch.float32 and norm.numel() == 1, where + ": norm")
+    types = {torch.float32: E2F_F32, torch.bfloat16: E2F_BF16}
+    for g, o in zip(grads, out):
+        _need(g.dtype in types and o.dtype == g.dtype and o.shape == g.shape and g.device == o.device == norm.device and
+              g.is_contiguous() and o.is_contiguous(), where)
+    pointers = ctypes.c_void_p * n
+    _check(_on(norm.device, load().e2f_grad_norm_clip, n, pointers(*[g.data_ptr() for g in grads]),
+               pointers(*[o.data_ptr() for o in out]), (ctypes.c_int64 * n)(*[g.numel() for g in grads]),
+               (ctypes.c_int32 * n)(*[types[g.dtype] for g in grads]), max_norm, norm.data_ptr(),
+               *_bytes_of(ws, norm, where + ": ws")), where)
 
 
 def e2f_profile_begin(ctx, max_calls):
