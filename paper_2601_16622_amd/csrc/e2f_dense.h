@@ -15,20 +15,30 @@
 
 namespace e2f {
 
-constexpr int DENSE_THREADS = 256;
-constexpr int DENSE_BM = 128;      // rows of a workgroup
 constexpr float LOG2E = 1.4426950408889634f;
+
+// What the score of a pair is formed from, in units of base-2 logarithms (so that the softmax's exponential is exp2).
+struct DenseScore {
+    float in;            // x = in * (q . k): the argument of the tanh, or without a cap the score itself
+    float out, inv_out2; // cap log2(e) and its square's reciprocal
+    float c[8];          // odd polynomial of out * tanh
+    int32_t capped, biased;
+};
 
 struct DenseParams {
     Rows q, k, v, out;             // out: out, or grad_q
     Rows go, gk, gv;               // backward: dL/dout, grad_k, grad_v
     const int32_t *q_offsets, *k_offsets, *q_lengths, *k_lengths;
     const float *q_pos, *k_pos, *slope;
-    int32_t Nq, Nk, S, Hk, group, D;
-    float scale, cap;
-    float4* stats;                 // backward: [Nq][Hq] softmax reference (base 2), 1 / sum, delta
+    int32_t Nq, Nk, S, Hk, group, D, group_shift;
+    uint32_t group_magic;
+    float scale;
+    DenseScore score;
+    float *part, *part_sum;        // forward with split keys: [splits][Nq][Hq][D] sums over a part's keys, [splits][Nq][Hq][2] reference, sum
+    float4* stats;                 // backward: [Nq][Hq] softmax reference, 1 / sum, delta
     float *slope_part;             // [Nq][Hq]
     float *q_pos_part, *k_pos_part;   // [Hq][Nq][3], [Hk][Nk][3]
+    __device__ __forceinline__ int over_group(uint32_t r) const { return (int)((uint64_t)r * group_magic >> group_shift); }
 };
 
 // The tokens of segment s that count: first token and number.
@@ -60,7 +70,20 @@ __device__ __forceinline__ int segment_of(const int32_t* offsets, int S, int N, 
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// Matrix instructions and operands of the two feature types.  DP: D rounded up to 32, zero beyond D.
+// The last segment that starts at or before a token.
+__device__ __forceinline__ int token_segment(const int32_t* offsets, int S, int token) {
+    int lo = 0, hi = S;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (offsets[mid] <= token) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// Matrix instructions and operands of the two feature types.  DP: D rounded up to 32, zero beyond D.  A tile is BN rows of
+// features in LDS, LD elements from row to row.
 template <typename T, int DP>
 struct Mma;
 
@@ -68,7 +91,7 @@ struct Mma;
 template <int DP>
 struct Mma<uint16_t, DP> {
     using T = uint16_t;
-    static constexpr int STEPS = DP / 16, BN = 64, LD = DP + 8, LDT = BN + 8;
+    static constexpr int STEPS = DP / 16, LD = DP + 8;
     // a row of features as an operand, for products over the features
     struct Frag {
         bf16x8 x[STEPS];
@@ -82,7 +105,7 @@ struct Mma<uint16_t, DP> {
             f.x[c] = __builtin_bit_cast(bf16x8, x);
         }
     }
-    // C += A B^T over the features: A 32 rows of a tile in LDS
+    // A B^T over the features: A 32 rows of a tile
     static __device__ __forceinline__ f32x16 dot(const T* tile, int row0, const Frag& b, int lane) {
         f32x16 acc = {};
         const T* p = tile + (row0 + (lane & 31)) * LD + 8 * (lane >> 5);
@@ -106,30 +129,21 @@ struct Mma<uint16_t, DP> {
         }
         return w;
     }
-    // acc[dt] += (features dt*32.. of the tile, transposed) W over the 32 tile rows from row0; `turned` is the transposed tile
-    static __device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const T*, const T* turned, int row0, const Weights& w, int lane) {
-        const T* p = turned + (lane & 31) * LDT + row0 + 4 * (lane >> 5);
+    // acc[dt] += (features 32 dt .. of the tile, transposed) W over the 32 tile rows from row0.  ds_read_b64_tr_b16 turns 4 rows of 16
+    // features in each 16 lanes: lane 4 r + c of them addresses features 4 c .. of row r, lane i gets feature i of the four rows.
+    static __device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const T* tile, int row0, const Weights& w, int lane) {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4* lds4;
+        const T* p = tile + (row0 + 4 * (lane >> 5) + ((lane >> 2) & 3)) * LD + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 #pragma unroll
         for (int dt = 0; dt < DP / 32; ++dt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const u32x2 a = *reinterpret_cast<const u32x2*>(p + dt * 32 * LDT + 16 * c);
-                const u32x2 b = *reinterpret_cast<const u32x2*>(p + dt * 32 * LDT + 16 * c + 8);
-                const u32x4 ab = {a[0], a[1], b[0], b[1]};
+                const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + dt * 32 + 16 * c * LD));
+                const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + dt * 32 + (16 * c + 8) * LD));
+                const auto ab = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
                 acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ab), w.x[c], acc[dt], 0, 0, 0);
             }
-    }
-    static constexpr int TILE = BN * LD, TURNED = DP * LDT;
-    // four rows of eight features to the transposed tile
-    static __device__ __forceinline__ void turn(T* turned, int row, int d, const u32x4 (&r)[4]) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            // two features of four rows each
-            const u32x2 even = {__builtin_amdgcn_perm(r[1][e], r[0][e], 0x05040100), __builtin_amdgcn_perm(r[3][e], r[2][e], 0x05040100)};
-            const u32x2 odd = {__builtin_amdgcn_perm(r[1][e], r[0][e], 0x07060302), __builtin_amdgcn_perm(r[3][e], r[2][e], 0x07060302)};
-            *reinterpret_cast<u32x2*>(turned + (d + 2 * e) * LDT + row) = even;
-            *reinterpret_cast<u32x2*>(turned + (d + 2 * e + 1) * LDT + row) = odd;
-        }
     }
 };
 
@@ -138,7 +152,7 @@ struct Mma<uint16_t, DP> {
 template <int DP>
 struct Mma<float, DP> {
     using T = float;
-    static constexpr int BN = 32, LD = DP + 8, LDT = 0, H = DP / 2;
+    static constexpr int LD = DP + 8, H = DP / 2;
     struct Frag {
         float x[H];
     };
@@ -167,7 +181,7 @@ struct Mma<float, DP> {
         f32x16 x;
     };
     static __device__ __forceinline__ Weights weights(const f32x16& p) { return Weights{p}; }
-    static __device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const T* tile, const T*, int row0, const Weights& w, int lane) {
+    static __device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const T* tile, int row0, const Weights& w, int lane) {
         const T* p = tile + (row0 + 4 * (lane >> 5)) * LD + (lane & 31);
 #pragma unroll
         for (int dt = 0; dt < DP / 32; ++dt)
@@ -175,45 +189,149 @@ struct Mma<float, DP> {
             for (int i = 0; i < 16; ++i)
                 acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(p[(8 * (i / 4) + i % 4) * LD + dt * 32], w.x[i], acc[dt], 0, 0, 0);
     }
-    static constexpr int TILE = BN * LD, TURNED = 0;
 };
 
-// BN rows of a tile from memory into LDS, rows and features behind the end as zeros; PLAIN, TURNED: which of the two forms.
-// row_at(r): the row's memory.
-template <typename M, int DP, bool PLAIN, bool TURNED, class RowAt>
-__device__ __forceinline__ void stage(typename M::T* plain, typename M::T* turned, int n, int D, RowAt row_at) {
+// BN rows of features on their way from memory into a tile, in the registers of THREADS threads: rows and features behind the end as zeros.
+template <typename M, int DP, int BN, int THREADS>
+struct Transfer {
     using T = typename M::T;
-    constexpr int V = 16 / sizeof(T);
-    if constexpr (sizeof(T) == 4 || !TURNED) {
-        constexpr int VECS = DP / V;
-        for (int i = threadIdx.x; i < M::BN * VECS; i += DENSE_THREADS) {
-            const int r = i / VECS, d = i % VECS * V;
-            u32x4 x = {0, 0, 0, 0};
-            if (r < n && d < D) x = *reinterpret_cast<const u32x4*>(row_at(r) + d * sizeof(T));
-            *reinterpret_cast<u32x4*>(plain + r * M::LD + d) = x;
-        }
-    } else {
-        constexpr int VECS = DP / 8;
-        for (int i = threadIdx.x; i < M::BN / 4 * VECS; i += DENSE_THREADS) {
-            const int r = i / VECS * 4, d = i % VECS * 8;
-            u32x4 x[4];
+    static constexpr int V = 16 / sizeof(T), VECS = DP / V, EACH = BN * VECS / THREADS;
+    static_assert(BN * VECS % THREADS == 0, "whole vectors for each thread");
+    u32x4 x[EACH];
+    // row_at(r): the memory of row r
+    template <class RowAt>
+    __device__ __forceinline__ void load(int tid, int n, int D, RowAt row_at) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[e] = u32x4{0, 0, 0, 0};
-                if (r + e < n && d < D) x[e] = *reinterpret_cast<const u32x4*>(row_at(r + e) + d * 2);
-                if (PLAIN) *reinterpret_cast<u32x4*>(plain + (r + e) * M::LD + d) = x[e];
+        for (int j = 0; j < EACH; ++j) {
+            const int i = tid + j * THREADS, r = i / VECS, d = i % VECS * V;
+            x[j] = u32x4{0, 0, 0, 0};
+            if (r < n && d < D) x[j] = *reinterpret_cast<const u32x4*>(row_at(r) + d * sizeof(T));
+        }
+    }
+    __device__ __forceinline__ void store(int tid, T* tile) const {
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            const int i = tid + j * THREADS;
+            *reinterpret_cast<u32x4*>(tile + i / VECS * M::LD + i % VECS * V) = x[j];
+        }
+    }
+};
+
+// The places of BN tokens likewise, into three lines of BN.
+template <int BN, int THREADS>
+struct PlaceTransfer {
+    static constexpr int EACH = (3 * BN + THREADS - 1) / THREADS;
+    float x[EACH];
+    __device__ __forceinline__ void load(int tid, int n, const float* pos) {
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            const int i = tid + j * THREADS;
+            x[j] = i < 3 * n ? pos[i] : 0.0f;
+        }
+    }
+    __device__ __forceinline__ void store(int tid, float* place) const {
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            const int i = tid + j * THREADS;
+            if (i < 3 * BN) place[i % 3 * BN + i / 3] = x[j];
+        }
+    }
+};
+
+// Orders a tile's stores before the reads of it (and those before the next stores): of a whole workgroup, or of one wave alone.
+template <bool WORKGROUP>
+__device__ __forceinline__ void tile_sync() {
+    if constexpr (WORKGROUP) {
+        __syncthreads();
+    } else {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// p (products q . k) -> scores minus base; SLACK: slack = 1 - tanh^2.  The tanh of an argument x up to 1 is an odd polynomial (relative
+// error 8e-8; scores are rarely near their cap), beyond that 1 - 2 / (1 + e^2x), whose absolute error of 1e-7 is then a relative one.
+// Which form an element gets goes by the element alone, so that a row's result does not depend on the rows beside it; the
+// vote only leaves the second form out where no element of the wave needs it.
+template <bool SLACK>
+__device__ __forceinline__ void cap_scores(f32x16& p, f32x16& slack, const DenseScore& A, float base) {
+    if (!A.capped) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = p[i] * A.in - base;
+        if (SLACK) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) slack[i] = 1.0f;
+        }
+        return;
+    }
+    float far = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        p[i] *= A.in;
+        far = fmaxf(far, fabsf(p[i]));
+    }
+    auto polynomial = [&](float x) {
+        const float y = x * x;
+        float t = A.c[7];
+#pragma unroll
+        for (int k = 6; k >= 0; --k) t = t * y + A.c[k];
+        return t;
+    };
+    auto near = [&](int i) {
+        const float x = p[i], t = polynomial(x);
+        if (SLACK) {
+            const float v = x * t;
+            slack[i] = 1.0f - v * A.inv_out2 * v;
+        }
+        p[i] = x * t - base;
+    };
+    if (!__any(far > 1.0f)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) near(i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float x = p[i], r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f * LOG2E)));
+            near(i);
+            if (fabsf(x) > 1.0f) {
+                if (SLACK) slack[i] = 4.0f * r * (1.0f - r);       // 1 - (1 - 2 r)^2
+                p[i] = (1.0f - 2.0f * r) * A.out - base;
             }
-            M::turn(turned, r, d, x);
         }
     }
 }
 
-// Places of BN tokens, as three lines.
+// The running reference of a row's softmax moves to the first tile's maximum, and later when scores pass it by 2^8 (sums of weights up to
+// 2^8 lose nothing in binary32 or bf16), so that the sums are rescaled rarely.  p holds scores minus base and gets those minus the new
+// reference.  Returns whether any row's moved; `shrink` is then the factor of what a row has summed so far.
+__device__ __forceinline__ float reference_base(float top) { return top > -INFINITY ? top : 0.0f; }
+__device__ __forceinline__ bool move_reference(f32x16& p, float& top, float& shrink) {
+    float most = p[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) most = fmaxf(most, p[i]);
+    most = fmaxf(most, other_half(most));
+    const bool unset = top == -INFINITY, moves = unset ? most > -INFINITY : most > 8.0f;
+    if (!__any(moves)) return false;
+    const float up = moves ? most : 0.0f;
+    shrink = !moves ? 1.0f : unset ? 0.0f : __builtin_amdgcn_exp2f(-up);
+    if (moves) top = reference_base(top) + up;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p[i] -= up;
+    return true;
+}
+
+// p -= slope * distance; the places of the tile's rows lie in three lines of BN, `at` the lane's first row.
 template <int BN>
-__device__ __forceinline__ void stage_places(float* s, const float* pos, int64_t first, int n) {
-    for (int i = threadIdx.x; i < 3 * BN; i += DENSE_THREADS) {
-        const int r = i / 3, c = i % 3;
-        s[c * BN + r] = r < n ? pos[first * 3 + i] : 0.0f;
+__device__ __forceinline__ void bias_scores(f32x16& p, float x, float y, float z, float slope, const float* place, int at) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const f32x4 px = *reinterpret_cast<const f32x4*>(place + at + 8 * b), py = *reinterpret_cast<const f32x4*>(place + BN + at + 8 * b),
+                    pz = *reinterpret_cast<const f32x4*>(place + 2 * BN + at + 8 * b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float dx = x - px[e], dy = y - py[e], dz = z - pz[e];
+            p[4 * b + e] -= slope * __builtin_amdgcn_sqrtf(dx * dx + dy * dy + dz * dz);
+        }
     }
 }
 
@@ -238,6 +356,5 @@ __device__ __forceinline__ void store_row(char* row, const f32x16 (&acc)[DP / 32
         }
 }
 
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
 
 }  // namespace e2f

@@ -1,90 +1,246 @@
 // Attention among all atoms of a segment, forward: one pass over the keys with the running maximum and sum of the softmax.
 #include "e2f_dense_api.h"
-#include "e2f_dense.h"
 
 namespace {
 
 using namespace e2f;
 
-template <typename T, int DP>
-__global__ __launch_bounds__(DENSE_THREADS) void k_dense_fwd(DenseParams A) {
+// ROWW waves of a workgroup own 32 rows each and share a tile of keys; or KEYW waves own the same 32 rows, take turns at
+// the tiles (each with LDS of its own) and join at the end.  Workgroups with the same blockIdx.x and another blockIdx.y take
+// parts of the keys, joined by k_dense_join.
+template <typename T, int DP, int ROWW, int KEYW>
+struct FwdShape {
     using M = Mma<T, DP>;
-    constexpr int BN = M::BN;
-    __shared__ __align__(16) T ks[M::TILE];
-    __shared__ __align__(16) T vs[sizeof(T) == 4 ? M::TILE : M::TURNED];
-    __shared__ __align__(16) float place[3 * BN];
+    static constexpr int BN = ROWW > 1 && sizeof(T) == 2 ? 64 : 32, BM = 32 * ROWW, THREADS = 64 * ROWW * KEYW, STAGERS = 64 * ROWW;
+    struct Tile {
+        T k[BN * M::LD], v[BN * M::LD];
+        float place[3 * BN];
+    };
+};
+
+template <typename T, int DP, int ROWW, int KEYW>
+__global__ __launch_bounds__(64 * ROWW * KEYW) void k_dense_fwd(DenseParams A) {
+    using F = FwdShape<T, DP, ROWW, KEYW>;
+    using M = typename F::M;
+    constexpr int BN = F::BN;
+    __shared__ __align__(16) typename F::Tile tiles[KEYW];
+    __shared__ float joint[KEYW > 1 ? KEYW : 1][2][32];
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
+    const int roww = ROWW > 1 ? wave : 0, keyw = KEYW > 1 ? wave : 0, tid = KEYW > 1 ? lane : threadIdx.x;
+    typename F::Tile& tile = tiles[keyw];
     const int head_k = blockIdx.x % A.Hk;
-    const int64_t tile = blockIdx.x / A.Hk;
-    const int s = segment_of(A.q_offsets, A.S, A.Nq, A.group, DENSE_BM, tile);
+    const int64_t t_index = blockIdx.x / A.Hk;
+    const int s = segment_of(A.q_offsets, A.S, A.Nq, A.group, F::BM, t_index);
     int q0, nq, k0, nk;
     segment_range(A.q_offsets, A.q_lengths, s, A.Nq, q0, nq);
     segment_range(A.k_offsets, A.k_lengths, s, A.Nk, k0, nk);
-    const int64_t row0 = (tile - first_tile(A.q_offsets, s, A.Nq, A.group, DENSE_BM)) * DENSE_BM, rows = (int64_t)nq * A.group;
+    const int64_t row0 = (t_index - first_tile(A.q_offsets, s, A.Nq, A.group, F::BM)) * F::BM, rows = (int64_t)nq * A.group;
     if (row0 < 0 || row0 >= rows) return;
-    const int64_t row = row0 + wave * 32 + (lane & 31);
-    const bool valid = row < rows, busy = row0 + wave * 32 < rows;
-    const int query = q0 + (valid ? (int)(row / A.group) : 0), head = head_k * A.group + (valid ? (int)(row % A.group) : 0);
+    const int64_t row = row0 + roww * 32 + (lane & 31);
+    const bool valid = row < rows, busy = row0 + roww * 32 < rows;
+    const int in_segment = valid ? A.over_group((uint32_t)row) : 0;
+    const int query = q0 + in_segment, head = head_k * A.group + (valid ? (int)row - in_segment * A.group : 0);
+    // this workgroup's part of the keys, in whole tiles
+    const int parts = gridDim.y, n_tiles = (nk + BN - 1) / BN, each = (n_tiles + parts - 1) / parts;
+    const int begin = min((int64_t)nk, (int64_t)blockIdx.y * each * BN), end = min((int64_t)nk, (int64_t)begin + (int64_t)each * BN);
     typename M::Frag qf;
     M::load(qf, A.q.row(query, head), A.D, valid, half);
     float x = 0, y = 0, z = 0, slope = 0;
-    if (A.slope) {
+    if (A.score.biased) {
         x = A.q_pos[(int64_t)query * 3];
         y = A.q_pos[(int64_t)query * 3 + 1];
         z = A.q_pos[(int64_t)query * 3 + 2];
         slope = A.slope[head] * LOG2E;
     }
-    const float in = A.cap > 0 ? A.scale / A.cap : A.scale * LOG2E, out = A.cap * LOG2E;
     f32x16 acc[DP / 32] = {};
     float top = -INFINITY, sum = 0;
-    for (int t = 0; t < nk; t += BN) {
-        const int n = min(BN, nk - t);
-        __syncthreads();
-        stage<M, DP, true, false>(ks, nullptr, n, A.D, [&](int r) { return A.k.row(k0 + t + r, head_k); });
-        if constexpr (sizeof(T) == 4) stage<M, DP, true, false>(vs, nullptr, n, A.D, [&](int r) { return A.v.row(k0 + t + r, head_k); });
-        else stage<M, DP, false, true>(nullptr, vs, n, A.D, [&](int r) { return A.v.row(k0 + t + r, head_k); });
-        if (A.slope) stage_places<BN>(place, A.k_pos, k0 + t, n);
-        __syncthreads();
+    Transfer<M, DP, BN, F::STAGERS> tk, tv;
+    PlaceTransfer<BN, F::STAGERS> tp;
+    auto fetch = [&](int t) {
+        const int n = end - t;
+        tk.load(tid, n, A.D, [&](int r) { return A.k.row(k0 + t + r, head_k); });
+        tv.load(tid, n, A.D, [&](int r) { return A.v.row(k0 + t + r, head_k); });
+        if (A.score.biased) tp.load(tid, min(n, BN), A.k_pos + (int64_t)(k0 + t) * 3);
+    };
+    const int first = begin + keyw * BN;
+    if (first < end) fetch(first);
+    for (int t = first; t < end; t += KEYW * BN) {
+        tile_sync<(ROWW > 1)>();
+        tk.store(tid, tile.k);
+        tv.store(tid, tile.v);
+        if (A.score.biased) tp.store(tid, tile.place);
+        tile_sync<(ROWW > 1)>();
+        if (t + KEYW * BN < end) fetch(t + KEYW * BN);
         if (!busy) continue;
+        const int n = min(BN, end - t);
         for (int m = 0; m < n; m += 32) {
-            f32x16 p = M::dot(ks, m, qf, lane);
-            float most = -INFINITY;
+            f32x16 p = M::dot(tile.k, m, qf, lane);
+            cap_scores<false>(p, p, A.score, reference_base(top));
+            if (A.score.biased) bias_scores<BN>(p, x, y, z, slope, tile.place, m + 4 * half);
+            if (n - m < 32) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (m + 8 * (i / 4) + 4 * half + i % 4 >= n) p[i] = -INFINITY;
+            }
+            float shrink;
+            if (move_reference(p, top, shrink)) {
+                sum *= shrink;
+#pragma unroll
+                for (int dt = 0; dt < DP / 32; ++dt) acc[dt] *= shrink;
+            }
+            float add = 0;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const int key = m + 8 * (i / 4) + 4 * half + i % 4;
-                float v = p[i] * in;
-                if (A.cap > 0) v = tanhf(v) * out;
-                if (A.slope) {
-                    const float dx = x - place[key], dy = y - place[BN + key], dz = z - place[2 * BN + key];
-                    v -= slope * sqrtf(dx * dx + dy * dy + dz * dz);
-                }
-                p[i] = key < n ? v : -INFINITY;
-                most = fmaxf(most, p[i]);
+                p[i] = __builtin_amdgcn_exp2f(p[i]);
+                add += p[i];
             }
-            most = fmaxf(most, other_half(most));
-            const float now = fmaxf(top, most), shrink = exp2f(top - now);
-            top = now;
-            sum *= shrink;
-#pragma unroll
-            for (int dt = 0; dt < DP / 32; ++dt) acc[dt] *= shrink;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                p[i] = exp2f(p[i] - top);
-                sum += p[i];
-            }
-            M::accumulate(acc, vs, vs, m, M::weights(p), lane);
+            sum += add;
+            M::accumulate(acc, tile.v, m, M::weights(p), lane);
         }
     }
     sum += other_half(sum);
-    if (valid) store_row<T, DP>(A.out.row(query, head), acc, nk > 0 ? 1.0f / sum : 0.0f, A.D, half);
+    if constexpr (KEYW > 1) {
+        // over the waves, in order; a wave without keys has a reference of -inf and a sum of 0
+        joint[keyw][0][lane & 31] = top;
+        joint[keyw][1][lane & 31] = sum;
+        __syncthreads();
+        float best = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < KEYW; ++w) best = fmaxf(best, joint[w][0][lane & 31]);
+        const float mine = best > -INFINITY ? __builtin_amdgcn_exp2f(top - best) : 0.0f;
+        float total = 0;
+#pragma unroll
+        for (int w = 0; w < KEYW; ++w)
+            total += joint[w][1][lane & 31] * (best > -INFINITY ? __builtin_amdgcn_exp2f(joint[w][0][lane & 31] - best) : 0.0f);
+        float* all = reinterpret_cast<float*>(tiles);       // [KEYW][16][64] of one 32 x 32 block at a time
+        static_assert(sizeof(tiles) >= KEYW * 1024 * 4, "room for a block of every wave");
+#pragma unroll
+        for (int dt = 0; dt < DP / 32; ++dt) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) all[(keyw * 16 + i) * 64 + lane] = acc[dt][i] * mine;
+            __syncthreads();
+            if (keyw == 0) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    float a = all[i * 64 + lane];
+#pragma unroll
+                    for (int w = 1; w < KEYW; ++w) a += all[(w * 16 + i) * 64 + lane];
+                    acc[dt][i] = a;
+                }
+            }
+        }
+        top = best;
+        sum = total;
+        if (keyw != 0) return;
+    }
+    if (!valid) return;
+    if (parts == 1) {
+        store_row<T, DP>(A.out.row(query, head), acc, nk > 0 ? 1.0f / sum : 0.0f, A.D, half);
+    } else {
+        const int64_t at = ((int64_t)blockIdx.y * A.Nq + query) * (A.Hk * A.group) + head;
+        if (begin < end) store_row<float, DP>(reinterpret_cast<char*>(A.part + at * A.D), acc, 1.0f, A.D, half);
+        if (half == 0) {
+            A.part_sum[at * 2] = begin < end ? top : -INFINITY;
+            A.part_sum[at * 2 + 1] = begin < end ? sum : 0.0f;
+        }
+    }
+}
+
+// Joins the parts of a row: out = sum_p 2^(top_p - top) part_p / sum_p 2^(top_p - top) sum_p.  A workgroup for a row, its waves
+// take turns at the parts.
+constexpr int JOIN_WAVES = 4;
+template <typename T>
+__global__ __launch_bounds__(64 * JOIN_WAVES) void k_dense_join(DenseParams A, int parts) {
+    __shared__ float sums[JOIN_WAVES][128], weight[JOIN_WAVES];
+    const int Hq = A.Hk * A.group, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row = blockIdx.x, stride = (int64_t)A.Nq * Hq;
+    const int query = (int)(row / Hq);
+    int first, n, s = token_segment(A.q_offsets, A.S, query);
+    segment_range(A.q_offsets, A.q_lengths, s, A.Nq, first, n);
+    if (query < first || query >= first + n) return;
+    float top = -INFINITY;
+    for (int p = lane; p < parts; p += 64) top = fmaxf(top, A.part_sum[(p * stride + row) * 2]);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    float a0 = 0, a1 = 0, sum = 0;
+    for (int p = wave; p < parts; p += JOIN_WAVES) {
+        const float t = A.part_sum[(p * stride + row) * 2];
+        if (!(A.part_sum[(p * stride + row) * 2 + 1] != 0.0f)) continue;     // no keys in this part (a NaN counts)
+        const float f = __builtin_amdgcn_exp2f(t - top);
+        const float* part = A.part + (p * stride + row) * A.D;
+        sum += f * A.part_sum[(p * stride + row) * 2 + 1];
+        if (lane < A.D) a0 += f * part[lane];
+        if (lane + 64 < A.D) a1 += f * part[lane + 64];
+    }
+    sums[wave][lane] = a0;
+    sums[wave][lane + 64] = a1;
+    if (lane == 0) weight[wave] = sum;
+    __syncthreads();
+    if (wave > 0) return;
+    int k_first, nk;
+    segment_range(A.k_offsets, A.k_lengths, s, A.Nk, k_first, nk);
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < JOIN_WAVES; ++w) sum += weight[w];
+    char* out = A.out.row(query, row % Hq);
+    for (int d = lane; d < A.D; d += 64) {
+        float a = 0;
+#pragma unroll
+        for (int w = 0; w < JOIN_WAVES; ++w) a += sums[w][d];
+        a = nk > 0 ? a / sum : 0.0f;
+        if constexpr (sizeof(T) == 4) reinterpret_cast<float*>(out)[d] = a;
+        else reinterpret_cast<uint16_t*>(out)[d] = (uint16_t)pack_bf16(a, 0.0f);
+    }
+}
+
+// Which form runs, from the sizes that the host knows.
+struct FwdPlan {
+    int roww, keyw, parts;
+    int64_t tiles;
+};
+FwdPlan fwd_plan(const e2f_dense_args* a) {
+    FwdPlan P = {4, 1, 1, 0};
+    const int group = a->Hq / a->Hk;
+    const int64_t rows = (int64_t)a->Nq * group, S = a->S > 0 ? a->S : 1;
+    if (rows <= 32 * S) {
+        P.roww = 1;
+        P.keyw = a->Nk > 128 * S ? 4 : 1;
+    }
+    P.tiles = dense_tiles(a->Nq, group, a->S, 32 * P.roww);
+    const int64_t have = P.tiles * a->Hk, want = 512, most = a->Nk / S / (64 * P.keyw);
+    int64_t parts = have > 0 ? want / have : 1;
+    if (parts > most) parts = most;
+    if (parts > 1024) parts = 1024;
+    if (parts > 1) P.parts = (int)parts;
+    return P;
+}
+
+template <typename T, int DP>
+void launch_dp(const DenseParams& A, const FwdPlan& P, hipStream_t st) {
+    const dim3 grid((unsigned)(P.tiles * A.Hk), (unsigned)P.parts);
+    if (P.roww == 4) k_dense_fwd<T, DP, 4, 1><<<grid, 256, 0, st>>>(A);
+    else if (P.keyw == 4) k_dense_fwd<T, DP, 1, 4><<<grid, 256, 0, st>>>(A);
+    else k_dense_fwd<T, DP, 1, 1><<<grid, 64, 0, st>>>(A);
+    if (P.parts > 1) k_dense_join<T><<<(unsigned)((int64_t)A.Nq * A.Hk * A.group), 64 * JOIN_WAVES, 0, st>>>(A, P.parts);
 }
 
 template <typename T>
-void launch(const DenseParams& A, unsigned blocks, hipStream_t st) {
-    if (A.D <= 32) k_dense_fwd<T, 32><<<blocks, DENSE_THREADS, 0, st>>>(A);
-    else if (A.D <= 64) k_dense_fwd<T, 64><<<blocks, DENSE_THREADS, 0, st>>>(A);
-    else if (A.D <= 96) k_dense_fwd<T, 96><<<blocks, DENSE_THREADS, 0, st>>>(A);
-    else k_dense_fwd<T, 128><<<blocks, DENSE_THREADS, 0, st>>>(A);
+void launch(const DenseParams& A, const FwdPlan& P, hipStream_t st) {
+    if (A.D <= 32) launch_dp<T, 32>(A, P, st);
+    else if (A.D <= 64) launch_dp<T, 64>(A, P, st);
+    else if (A.D <= 96) launch_dp<T, 96>(A, P, st);
+    else launch_dp<T, 128>(A, P, st);
+}
+
+size_t layout(const e2f_dense_args* a, const FwdPlan& P, char* ws, DenseParams* A) {
+    if (P.parts == 1) return 0;
+    const size_t rows = (size_t)P.parts * a->Nq * a->Hq, sums = e2f_align_up(rows * 2 * sizeof(float));
+    if (A) {
+        A->part_sum = reinterpret_cast<float*>(ws);
+        A->part = reinterpret_cast<float*>(ws + sums);
+    }
+    return sums + e2f_align_up(rows * a->D * sizeof(float));
 }
 
 }  // namespace
@@ -96,9 +252,10 @@ e2f_status dense_check_sizes(const e2f_dense_args* a) {
         a->D <= 0 || a->Hq % a->Hk || !isfinite(a->scale) || !(a->cap >= 0.0f) || !isfinite(a->cap))
         return E2F_ERR_INVALID_ARG;
     if (a->D % 8 || a->D > 128 || a->Hq > 1024) return E2F_ERR_UNSUPPORTED;
-    // the grid of either direction is a 31-bit number
+    // the grid of either direction and the stacked rows of a segment are 31-bit numbers
     const int64_t most = INT32_MAX / a->Hk;
-    if (dense_tiles(a->Nq, a->Hq / a->Hk, a->S, DENSE_BM) > most || dense_tiles(a->Nk, 1, a->S, DENSE_BM) > most)
+    if ((int64_t)a->Nq * (a->Hq / a->Hk) > INT32_MAX - 1024) return E2F_ERR_UNSUPPORTED;
+    if (dense_tiles(a->Nq, a->Hq / a->Hk, a->S, 32) > most || dense_tiles(a->Nk, 1, a->S, 32) > most)
         return E2F_ERR_UNSUPPORTED;
     return E2F_OK;
 }
@@ -128,9 +285,24 @@ void dense_fill(DenseParams& A, const e2f_dense_args* a, const e2f_heads* q, con
     A.S = a->S;
     A.Hk = a->Hk;
     A.group = a->Hq / a->Hk;
+    // r / group = r magic >> (31 + ceil(log2 group)) for 0 <= r < 2^31
+    int bits = 0;
+    while ((1 << bits) < A.group) ++bits;
+    A.group_shift = 31 + bits;
+    A.group_magic = (uint32_t)((1ull << A.group_shift) / A.group + 1);
     A.D = a->D;
     A.scale = a->scale;
-    A.cap = a->cap;
+    DenseScore& s = A.score;
+    s.capped = a->cap > 0.0f;
+    s.biased = a->slope != nullptr;
+    s.in = s.capped ? a->scale / a->cap : (float)((double)a->scale * 1.4426950408889634);
+    const double out = (double)a->cap * 1.4426950408889634;
+    s.out = (float)out;
+    s.inv_out2 = s.capped ? (float)(1.0 / (out * out)) : 0.0f;
+    // tanh x / x as a polynomial of x^2 on [0, 1], its relative error 4e-9 at most (minimised over the interval)
+    static const double tanh_c[8] = {0.99999999577764732,   -0.33333278673333597, 0.13332159672365009,    -0.053870912721773931,
+                                     0.021464820153790358, -0.0079174443902042118, 0.0022822293973515737, -0.00035334546706570396};
+    for (int i = 0; i < 8; ++i) s.c[i] = (float)(out * tanh_c[i]);
 }
 
 }  // namespace e2f
@@ -138,8 +310,7 @@ void dense_fill(DenseParams& A, const e2f_dense_args* a, const e2f_heads* q, con
 extern "C" {
 
 size_t e2f_dense_attn_workspace_bytes(const e2f_dense_args* a) {
-    (void)a;
-    return 0;
+    return dense_check_sizes(a) == E2F_OK ? layout(a, fwd_plan(a), nullptr, nullptr) : 0;
 }
 
 e2f_status e2f_dense_attn_forward(const e2f_dense_args* a, const e2f_heads* q, const e2f_heads* k, const e2f_heads* v,
@@ -150,7 +321,8 @@ e2f_status e2f_dense_attn_forward(const e2f_dense_args* a, const e2f_heads* q, c
         (rc = check_rows(v, a->dtype, a->Nk, a->Hk)) != E2F_OK ||
         (rc = check_result_rows(out, a->dtype, a->Nq, a->Hq, a->D)) != E2F_OK)
         return rc;
-    const size_t need = e2f_dense_attn_workspace_bytes(a);
+    const FwdPlan P = fwd_plan(a);
+    const size_t need = layout(a, P, nullptr, nullptr);
     if (need && (!ws || !aligned_ws(ws))) return E2F_ERR_INVALID_ARG;
     if (ws_bytes < need) return E2F_ERR_WORKSPACE_TOO_SMALL;
     if (a->Nq == 0 || a->S == 0) return E2F_OK;
@@ -158,9 +330,9 @@ e2f_status e2f_dense_attn_forward(const e2f_dense_args* a, const e2f_heads* q, c
     DenseParams A;
     dense_fill(A, a, q, k, v);
     A.out = rows_of(out, a->dtype);
-    const unsigned blocks = (unsigned)(dense_tiles(a->Nq, A.group, a->S, DENSE_BM) * a->Hk);
-    if (a->dtype == E2F_BF16) launch<uint16_t>(A, blocks, st);
-    else launch<float>(A, blocks, st);
+    layout(a, P, static_cast<char*>(ws), &A);
+    if (a->dtype == E2F_BF16) launch<uint16_t>(A, P, st);
+    else launch<float>(A, P, st);
     E2F_HIP_CHECK(hipGetLastError());
     return E2F_OK;
 }
