@@ -36,8 +36,10 @@ struct DenseParams {
     DenseScore score;
     float *part, *part_sum;        // forward with split keys: [splits][Nq][Hq][D] sums over a part's keys, [splits][Nq][Hq][2] reference, sum
     float4* stats;                 // backward: [Nq][Hq] softmax reference, 1 / sum, delta
-    float *slope_part;             // [Nq][Hq]
-    float *q_pos_part, *k_pos_part;   // [Hq][Nq][3], [Hk][Nk][3]
+    // of the parts of a backward pass: [parts] of [row tiles][Hq], [Hq][Nq][3], [Hk][Nk][3], [Nq][Hq], [Nq][Hq][D], [Nk][Hk][D]
+    float *slope_part, *q_pos_part, *k_pos_part;
+    float4* stats_part;
+    float *gq_part, *gk_part, *gv_part;
     __device__ __forceinline__ int over_group(uint32_t r) const { return (int)((uint64_t)r * group_magic >> group_shift); }
 };
 
@@ -299,6 +301,19 @@ __device__ __forceinline__ void cap_scores(f32x16& p, f32x16& slack, const Dense
             }
         }
     }
+}
+
+// The same with tanh x = 1 - 2 / (1 + e^2x) everywhere: 7 issue slots an element (the exponential and the reciprocal take two each)
+// where the polynomial and its vote take 11.  Its absolute error, 2^-23 of the cap, is for results in bf16 alone.
+__device__ __forceinline__ void cap_scores_coarse(f32x16& p, const DenseScore& A, float base) {
+    if (!A.capped) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = p[i] * A.in - base;
+        return;
+    }
+    const float in = A.in * (2.0f * LOG2E), out = -2.0f * A.out, over = A.out - base;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(p[i] * in)) * out + over;
 }
 
 // The running reference of a row's softmax moves to the first tile's maximum, and later when scores pass it by 2^8 (sums of weights up to

@@ -2,9 +2,9 @@
 //   delta_i = sum_j p dp;  ds = p (dp - delta);  dx = ds (1 - th^2)
 //   dv_j = sum_i p dout_i;  dq_i = scale sum_j dx k_j;  dk_j = scale sum_i dx q_i
 //   dslope_h = - sum ds d;  dr_i = - sum_{h,j} slope_h ds (r_i - r_j) / d,  dr_j the opposite
-// Nothing of a pair is stored: a kernel over rows forms the softmax statistics and delta in a first pass over the keys and
-// dq in a second one, a kernel over keys forms dk and dv, and each sum is formed by the workgroup that owns its row or key, so no
-// atomics are needed.  delta comes from the binary32 products and weights (not from the rounded result of the forward pass):
+// Nothing of a pair is stored: a kernel over rows forms the softmax statistics and delta, a second one dq, a kernel over keys
+// dk and dv.  Each sum is formed by the workgroup that owns its row or key, so no atomics are needed; where these are too few to
+// fill the chip the other side is cut into parts, whose sums are joined in their order.  delta comes from the binary32 products and weights (not from the rounded result of the forward pass):
 // the gradients of slope and places are binary32 and keep their precision.
 #include "e2f_dense_api.h"
 
@@ -12,6 +12,11 @@ namespace {
 
 using namespace e2f;
 
+#ifndef WANT
+#define WANT 4096
+#define RMINF (DP <= 96 || sizeof(T) == 2 ? 2 : 1)
+#define KMINF (DP * sizeof(T) <= 128 ? 2 : 1)
+#endif
 constexpr int SUM_THREADS = 256;
 
 // A distance and its reciprocal.  d^2 is kept from 0, so that a pair at one place has a finite reciprocal that the components of
@@ -22,73 +27,104 @@ __device__ __forceinline__ void distance(float dx, float dy, float dz, float& d,
     d = d2 * inv;
 }
 
+// A workgroup's 32 ROWW rows of a (segment, key head), its part of the segment's keys (blockIdx.y), and the walk over them.
 template <typename T, int DP, int ROWW>
-__global__ __launch_bounds__(64 * ROWW) void k_dense_bwd_rows(DenseParams A) {
+struct RowWalk {
     using M = Mma<T, DP>;
-    constexpr int BN = ROWW > 1 && sizeof(T) == 2 ? 64 : 32, BM = 32 * ROWW, THREADS = 64 * ROWW;
-    __shared__ __align__(16) T ks[BN * M::LD];
-    __shared__ __align__(16) T vs[BN * M::LD];
-    __shared__ __align__(16) float place[3 * BN];
-    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = tid >> 6;
-    const int head_k = blockIdx.x % A.Hk;
-    const int64_t tile = blockIdx.x / A.Hk;
-    const int s = segment_of(A.q_offsets, A.S, A.Nq, A.group, BM, tile);
-    int q0, nq, k0, nk;
-    segment_range(A.q_offsets, A.q_lengths, s, A.Nq, q0, nq);
-    segment_range(A.k_offsets, A.k_lengths, s, A.Nk, k0, nk);
-    const int64_t row0 = (tile - first_tile(A.q_offsets, s, A.Nq, A.group, BM)) * BM, rows = (int64_t)nq * A.group;
-    if (row0 < 0 || row0 >= rows) return;
-    const int64_t row = row0 + wave * 32 + (lane & 31);
-    const bool valid = row < rows, busy = row0 + wave * 32 < rows;
-    const int in_segment = valid ? A.over_group((uint32_t)row) : 0;
-    const int query = q0 + in_segment, head = head_k * A.group + (valid ? (int)row - in_segment * A.group : 0);
-    typename M::Frag qf, gf;
-    M::load(qf, A.q.row(query, head), A.D, valid, half);
-    M::load(gf, A.go.row(query, head), A.D, valid, half);
-    float x = 0, y = 0, z = 0, slope = 0;
-    if (A.score.biased) {
-        x = A.q_pos[(int64_t)query * 3];
-        y = A.q_pos[(int64_t)query * 3 + 1];
-        z = A.q_pos[(int64_t)query * 3 + 2];
-        slope = A.slope[head];
-    }
-    const float slope2 = slope * LOG2E;
-    Transfer<M, DP, BN, THREADS> tk, tv;
-    PlaceTransfer<BN, THREADS> tp;
-    auto fetch = [&](int t) {
-        const int n = nk - t;
-        tk.load(tid, n, A.D, [&](int r) { return A.k.row(k0 + t + r, head_k); });
-        tv.load(tid, n, A.D, [&](int r) { return A.v.row(k0 + t + r, head_k); });
-        if (A.score.biased) tp.load(tid, min(n, BN), A.k_pos + (int64_t)(k0 + t) * 3);
+    static constexpr int BN = ROWW > 1 && sizeof(T) == 2 ? 64 : 32, BM = 32 * ROWW, THREADS = 64 * ROWW;
+    struct Tile {
+        T k[BN * M::LD], v[BN * M::LD];
+        float place[3 * BN];
     };
-    // walks over the keys: body(first row of 32 in the tile, how many count)
-    auto walk = [&](auto body) {
-        if (nk > 0) fetch(0);
-        for (int t = 0; t < nk; t += BN) {
+    int lane, half, head_k, k0, begin, end, query, head, first_head;
+    int64_t at;            // of the row among [Nq][Hq]
+    bool any, valid, busy;
+    float x, y, z, slope;
+    typename M::Frag qf, gf;
+
+    __device__ __forceinline__ RowWalk(const DenseParams& A) {
+        lane = threadIdx.x & 63;
+        half = lane >> 5;
+        const int wave = threadIdx.x >> 6;
+        head_k = blockIdx.x % A.Hk;
+        const int64_t tile = blockIdx.x / A.Hk;
+        const int s = segment_of(A.q_offsets, A.S, A.Nq, A.group, BM, tile);
+        int q0, nq, nk;
+        segment_range(A.q_offsets, A.q_lengths, s, A.Nq, q0, nq);
+        segment_range(A.k_offsets, A.k_lengths, s, A.Nk, k0, nk);
+        const int64_t row0 = (tile - first_tile(A.q_offsets, s, A.Nq, A.group, BM)) * BM, rows = (int64_t)nq * A.group;
+        any = row0 >= 0 && row0 < rows;
+        if (!any) return;
+        first_head = (int)(row0 % A.group);
+        const int64_t row = row0 + wave * 32 + (lane & 31);
+        valid = row < rows;
+        busy = row0 + wave * 32 < rows;
+        const int in_segment = valid ? A.over_group((uint32_t)row) : 0;
+        query = q0 + in_segment;
+        head = head_k * A.group + (valid ? (int)row - in_segment * A.group : 0);
+        at = (int64_t)query * (A.Hk * A.group) + head;
+        const int tiles = (nk + BN - 1) / BN, each = (tiles + (int)gridDim.y - 1) / (int)gridDim.y;
+        begin = (int)min((int64_t)nk, (int64_t)blockIdx.y * each * BN);
+        end = (int)min((int64_t)nk, (int64_t)begin + (int64_t)each * BN);
+        M::load(qf, A.q.row(query, head), A.D, valid, half);
+        M::load(gf, A.go.row(query, head), A.D, valid, half);
+        x = y = z = slope = 0;
+        if (A.score.biased) {
+            x = A.q_pos[(int64_t)query * 3];
+            y = A.q_pos[(int64_t)query * 3 + 1];
+            z = A.q_pos[(int64_t)query * 3 + 2];
+            slope = A.slope[head];
+        }
+    }
+    // body(first row of 32 keys in the tile, how many of them count)
+    template <class Body>
+    __device__ __forceinline__ void walk(const DenseParams& A, Tile& tile, Body body) {
+        const int tid = threadIdx.x;
+        Transfer<M, DP, BN, THREADS> tk, tv;
+        PlaceTransfer<BN, THREADS> tp;
+        auto fetch = [&](int t) {
+            const int n = end - t;
+            tk.load(tid, n, A.D, [&](int r) { return A.k.row(k0 + t + r, head_k); });
+            tv.load(tid, n, A.D, [&](int r) { return A.v.row(k0 + t + r, head_k); });
+            if (A.score.biased) tp.load(tid, min(n, BN), A.k_pos + (int64_t)(k0 + t) * 3);
+        };
+        if (begin < end) fetch(begin);
+        for (int t = begin; t < end; t += BN) {
             tile_sync<(ROWW > 1)>();
-            tk.store(tid, ks);
-            tv.store(tid, vs);
-            if (A.score.biased) tp.store(tid, place);
+            tk.store(tid, tile.k);
+            tv.store(tid, tile.v);
+            if (A.score.biased) tp.store(tid, tile.place);
             tile_sync<(ROWW > 1)>();
-            if (t + BN < nk) fetch(t + BN);
+            if (t + BN < end) fetch(t + BN);
             if (!busy) continue;
-            const int n = min(BN, nk - t);
+            const int n = min(BN, end - t);
             for (int m = 0; m < n; m += 32) body(m, n - m);
         }
-    };
-    auto behind = [&](f32x16& p, int n) {
+    }
+    // keys behind the end: weight 0
+    __device__ __forceinline__ void mask(f32x16& p, int n) const {
         if (n >= 32) return;
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             if (8 * (i / 4) + 4 * half + i % 4 >= n) p[i] = -INFINITY;
-    };
+    }
+};
+
+// Softmax statistics of the rows: reference, sum, sum of p dp.  With parts of the keys each leaves its own, [parts][Nq][Hq].
+template <typename T, int DP, int ROWW>
+__global__ __launch_bounds__(64 * ROWW, 2) void k_dense_bwd_stats(DenseParams A) {
+    using R = RowWalk<T, DP, ROWW>;
+    using M = typename R::M;
+    __shared__ __align__(16) typename R::Tile tile;
+    R w(A);
+    if (!w.any) return;
     float top = -INFINITY, sum = 0, delta = 0;
-    walk([&](int m, int n) {
-        f32x16 p = M::dot(ks, m, qf, lane);
-        const f32x16 dp = M::dot(vs, m, gf, lane);
+    w.walk(A, tile, [&](int m, int n) {
+        f32x16 p = M::dot(tile.k, m, w.qf, w.lane);
+        const f32x16 dp = M::dot(tile.v, m, w.gf, w.lane);
         cap_scores<false>(p, p, A.score, reference_base(top));
-        if (A.score.biased) bias_scores<BN>(p, x, y, z, slope2, place, m + 4 * half);
-        behind(p, n);
+        if (A.score.biased) bias_scores<R::BN>(p, w.x, w.y, w.z, w.slope * LOG2E, tile.place, m + 4 * w.half);
+        w.mask(p, n);
         float shrink;
         if (move_reference(p, top, shrink)) {
             sum *= shrink;
@@ -97,36 +133,75 @@ __global__ __launch_bounds__(64 * ROWW) void k_dense_bwd_rows(DenseParams A) {
         float add = 0, dot = 0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const float w = __builtin_amdgcn_exp2f(p[i]);
-            add += w;
-            dot += w * dp[i];
+            const float e = __builtin_amdgcn_exp2f(p[i]);
+            add += e;
+            dot += e * dp[i];
         }
         sum += add;
         delta += dot;
     });
     sum += other_half(sum);
     delta += other_half(delta);
-    const float inv = nk > 0 ? 1.0f / sum : 0.0f;
-    delta *= inv;
-    // weights stay without 1 / sum here: a row's sums get it at the end
+    if (!w.valid || w.half) return;
+    if (gridDim.y == 1) {
+        const float inv = w.begin < w.end ? 1.0f / sum : 0.0f;
+        A.stats[w.at] = make_float4(top, inv, delta * inv, 0.0f);
+    } else {
+        A.stats_part[(int64_t)blockIdx.y * A.Nq * (A.Hk * A.group) + w.at] = make_float4(top, sum, delta, 0.0f);
+    }
+}
+
+// Joins the parts' statistics.  Rows that no segment covers hold anything and are not read by anyone.
+__global__ __launch_bounds__(SUM_THREADS) void k_dense_bwd_join_stats(DenseParams A, int parts) {
+    const int64_t rows = (int64_t)A.Nq * (A.Hk * A.group), row = (int64_t)blockIdx.x * SUM_THREADS + threadIdx.x;
+    if (row >= rows) return;
+    float top = -INFINITY, sum = 0, delta = 0;
+    for (int p = 0; p < parts; ++p) top = fmaxf(top, A.stats_part[p * rows + row].x);
+    for (int p = 0; p < parts; ++p) {
+        const float4 s = A.stats_part[p * rows + row];
+        const float f = top > -INFINITY ? __builtin_amdgcn_exp2f(s.x - top) : 1.0f;
+        sum += f * s.y;
+        delta += f * s.z;
+    }
+    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;      // no keys: no weights
+    A.stats[row] = make_float4(top, inv, delta * inv, 0.0f);
+}
+
+// dq and a row's shares of the gradients of slope and place, from the statistics.
+template <typename T, int DP, int ROWW>
+__global__ __launch_bounds__(64 * ROWW, RMINF) void k_dense_bwd_rows(DenseParams A) {
+    using R = RowWalk<T, DP, ROWW>;
+    using M = typename R::M;
+    constexpr int BN = R::BN;
+    __shared__ __align__(16) typename R::Tile tile;
+    R w(A);
+    if (!w.any) {
+        if (A.slope_part)
+            for (int g = threadIdx.x; g < A.group; g += R::THREADS)
+                A.slope_part[((int64_t)blockIdx.y * (gridDim.x / A.Hk) + blockIdx.x / A.Hk) * (A.Hk * A.group) + w.head_k * A.group + g] = 0.0f;
+        return;
+    }
+    const float4 st = A.stats[w.at];
+    const float top = st.x, inv = st.y, delta = st.z, slope2 = w.slope * LOG2E;
+    // weights stay without 1 / sum: a row's sums get it at the end
     float dslope = 0, gx = 0, gy = 0, gz = 0;
     f32x16 acc[DP / 32] = {};
-    walk([&](int m, int n) {
-        f32x16 p = M::dot(ks, m, qf, lane), slack;
-        const f32x16 dp = M::dot(vs, m, gf, lane);
+    w.walk(A, tile, [&](int m, int n) {
+        f32x16 p = M::dot(tile.k, m, w.qf, w.lane), slack;
+        const f32x16 dp = M::dot(tile.v, m, w.gf, w.lane);
         cap_scores<true>(p, slack, A.score, top);
-        behind(p, n);
+        w.mask(p, n);
         if (A.score.biased) {
             float ts = 0, tx = 0, ty = 0, tz = 0;      // a tile's sums by themselves: shorter sums, smaller errors
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                const float* at = place + m + 4 * half + 8 * b;
+                const float* at = tile.place + m + 4 * w.half + 8 * b;
                 const f32x4 px = *reinterpret_cast<const f32x4*>(at), py = *reinterpret_cast<const f32x4*>(at + BN),
                             pz = *reinterpret_cast<const f32x4*>(at + 2 * BN);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int i = 4 * b + e;
-                    const float dx = x - px[e], dy = y - py[e], dz = z - pz[e];
+                    const float dx = w.x - px[e], dy = w.y - py[e], dz = w.z - pz[e];
                     float d, id;
                     distance(dx, dy, dz, d, id);
                     p[i] = __builtin_amdgcn_exp2f(p[i] - slope2 * d) * (dp[i] - delta);
@@ -149,23 +224,36 @@ __global__ __launch_bounds__(64 * ROWW) void k_dense_bwd_rows(DenseParams A) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) p[i] *= slack[i];
         }
-        M::accumulate(acc, ks, m, M::weights(p), lane);
+        M::accumulate(acc, tile.k, m, M::weights(p), w.lane);
     });
     dslope += other_half(dslope);
     gx += other_half(gx);
     gy += other_half(gy);
     gz += other_half(gz);
-    if (!valid) return;
-    store_row<T, DP>(A.out.row(query, head), acc, A.scale * inv, A.D, half);
-    if (half) return;
-    const int64_t at = (int64_t)query * (A.Hk * A.group) + head;
-    A.stats[at] = make_float4(top, inv, delta, 0.0f);
-    if (A.slope_part) A.slope_part[at] = -dslope * inv;
+    if (A.slope_part) {
+        // over the workgroup's rows, for each head of the group, in their order
+        __syncthreads();
+        float* rows = reinterpret_cast<float*>(&tile);
+        if (!w.half) rows[threadIdx.x / 64 * 32 + w.lane] = w.valid ? -dslope * inv : 0.0f;
+        __syncthreads();
+        const int first = w.first_head;       // of row 0 of the workgroup
+        for (int g = threadIdx.x; g < A.group; g += R::THREADS) {
+            float sum = 0;
+            for (int r = g >= first ? g - first : g - first + A.group; r < R::BM; r += A.group) sum += rows[r];
+            A.slope_part[((int64_t)blockIdx.y * (gridDim.x / A.Hk) + blockIdx.x / A.Hk) * (A.Hk * A.group) + w.head_k * A.group + g] = sum;
+        }
+    }
+    if (!w.valid) return;
+    const int Hq = A.Hk * A.group;
+    const int64_t at = (int64_t)blockIdx.y * A.Nq * Hq + w.at;
+    if (gridDim.y == 1) store_row<T, DP>(A.out.row(w.query, w.head), acc, A.scale * inv, A.D, w.half);
+    else store_row<float, DP>(reinterpret_cast<char*>(A.gq_part + at * A.D), acc, A.scale * inv, A.D, w.half);
+    if (w.half) return;
     if (A.q_pos_part) {
-        float* g = A.q_pos_part + ((int64_t)head * A.Nq + query) * 3;
-        g[0] = -slope * inv * gx;
-        g[1] = -slope * inv * gy;
-        g[2] = -slope * inv * gz;
+        float* g = A.q_pos_part + (((int64_t)blockIdx.y * Hq + w.head) * A.Nq + w.query) * 3;
+        g[0] = -w.slope * inv * gx;
+        g[1] = -w.slope * inv * gy;
+        g[2] = -w.slope * inv * gz;
     }
 }
 
@@ -173,7 +261,7 @@ __global__ __launch_bounds__(64 * ROWW) void k_dense_bwd_rows(DenseParams A) {
 enum { ROW_X, ROW_Y, ROW_Z, ROW_SLOPE, ROW_TOP, ROW_INV, ROW_DELTA, ROW_LINES };
 
 template <typename T, int DP, int ROWW>
-__global__ __launch_bounds__(64 * ROWW) void k_dense_bwd_keys(DenseParams A) {
+__global__ __launch_bounds__(64 * ROWW, KMINF) void k_dense_bwd_keys(DenseParams A) {
     using M = Mma<T, DP>;
     constexpr int BN = ROWW > 1 && sizeof(T) == 2 ? 64 : 32, BM = 32 * ROWW, THREADS = 64 * ROWW;
     __shared__ __align__(16) T qs[BN * M::LD];
@@ -201,11 +289,14 @@ __global__ __launch_bounds__(64 * ROWW) void k_dense_bwd_keys(DenseParams A) {
         y = A.k_pos[(int64_t)key * 3 + 1];
         z = A.k_pos[(int64_t)key * 3 + 2];
     }
+    // this workgroup's part of the rows
+    const int row_tiles = (rows + BN - 1) / BN, each = (row_tiles + (int)gridDim.y - 1) / (int)gridDim.y;
+    const int begin = (int)min((int64_t)rows, (int64_t)blockIdx.y * each * BN), end = (int)min((int64_t)rows, (int64_t)begin + (int64_t)each * BN);
     Transfer<M, DP, BN, THREADS> tq, tg;
     float4 st;
     float rx = 0, ry = 0, rz = 0, rs = 0;
     auto fetch = [&](int t) {
-        const int n = rows - t;
+        const int n = end - t;
         auto at = [&](const Rows& R, int r) {
             const int query = A.over_group((uint32_t)(t + r));
             return R.row(q0 + query, head_k * A.group + (t + r - query * A.group));
@@ -227,8 +318,8 @@ __global__ __launch_bounds__(64 * ROWW) void k_dense_bwd_keys(DenseParams A) {
     };
     float gx = 0, gy = 0, gz = 0;
     f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
-    if (rows > 0) fetch(0);
-    for (int t = 0; t < rows; t += BN) {
+    if (begin < end) fetch(begin);
+    for (int t = begin; t < end; t += BN) {
         tile_sync<(ROWW > 1)>();
         tq.store(tid, qs);
         tg.store(tid, gs);
@@ -242,9 +333,9 @@ __global__ __launch_bounds__(64 * ROWW) void k_dense_bwd_keys(DenseParams A) {
             par[ROW_DELTA][tid] = st.z;
         }
         tile_sync<(ROWW > 1)>();
-        if (t + BN < rows) fetch(t + BN);
+        if (t + BN < end) fetch(t + BN);
         if (!busy) continue;
-        const int n = min(BN, rows - t);
+        const int n = min(BN, end - t);
         for (int m = 0; m < n; m += 32) {
             f32x16 p = M::dot(qs, m, kf, lane), ds = M::dot(gs, m, vf, lane), slack;
             cap_scores<true>(p, slack, A.score, 0.0f);
@@ -292,35 +383,46 @@ __global__ __launch_bounds__(64 * ROWW) void k_dense_bwd_keys(DenseParams A) {
     gy += other_half(gy);
     gz += other_half(gz);
     if (!valid) return;
-    store_row<T, DP>(A.gk.row(key, head_k), dk, A.scale, A.D, half);
-    store_row<T, DP>(A.gv.row(key, head_k), dv, 1.0f, A.D, half);
+    if (gridDim.y == 1) {
+        store_row<T, DP>(A.gk.row(key, head_k), dk, A.scale, A.D, half);
+        store_row<T, DP>(A.gv.row(key, head_k), dv, 1.0f, A.D, half);
+    } else {
+        const int64_t at = (((int64_t)blockIdx.y * A.Nk + key) * A.Hk + head_k) * A.D;
+        store_row<float, DP>(reinterpret_cast<char*>(A.gk_part + at), dk, A.scale, A.D, half);
+        store_row<float, DP>(reinterpret_cast<char*>(A.gv_part + at), dv, 1.0f, A.D, half);
+    }
     if (A.k_pos_part && !half) {
-        float* g = A.k_pos_part + ((int64_t)head_k * A.Nk + key) * 3;
+        float* g = A.k_pos_part + (((int64_t)blockIdx.y * A.Hk + head_k) * A.Nk + key) * 3;
         g[0] = gx;
         g[1] = gy;
         g[2] = gz;
     }
 }
 
-// Sums of the partial place gradients over the heads, for the tokens that a segment's length covers, and of the slopes'
-// over the rows.  Workgroups: first those of the queries, then of the keys (a thread for a token), then one for each slope.
-__global__ __launch_bounds__(SUM_THREADS) void k_dense_bwd_sums(DenseParams A, float* gq, float* gk, float* gslope, int q_blocks, int k_blocks) {
+// Whether a segment's length covers a token.
+__device__ __forceinline__ bool covered(const int32_t* offsets, const int32_t* lengths, int S, int N, int token) {
+    int first, n;
+    segment_range(offsets, lengths, token_segment(offsets, S, token), N, first, n);
+    return token >= first && token < first + n;
+}
+
+// Sums of what parts and heads left of the gradients of places, for the covered tokens, and of the slopes' over the workgroups.
+// Workgroups: first those of the queries, then of the keys (a thread for a token), then one for each slope.
+__global__ __launch_bounds__(SUM_THREADS) void k_dense_bwd_sums(DenseParams A, float* gq, float* gk, float* gslope, int q_blocks, int k_blocks,
+                                                                int row_parts, int key_parts, int64_t slope_lines) {
     const int Hq = A.Hk * A.group;
     int b = blockIdx.x;
     if (b < q_blocks + k_blocks) {
         const bool keys = b >= q_blocks;
         if (keys) b -= q_blocks;
-        const int N = keys ? A.Nk : A.Nq, H = keys ? A.Hk : Hq;
-        const int32_t* offsets = keys ? A.k_offsets : A.q_offsets;
+        const int N = keys ? A.Nk : A.Nq, planes = keys ? A.Hk * key_parts : Hq * row_parts;
         const float* part = keys ? A.k_pos_part : A.q_pos_part;
         float* g = keys ? gk : gq;
         const int64_t token = (int64_t)b * SUM_THREADS + threadIdx.x;
         if (token >= N) return;
-        int first, n;
-        segment_range(offsets, keys ? A.k_lengths : A.q_lengths, token_segment(offsets, A.S, (int)token), N, first, n);
-        if (token < first || token >= first + n) return;
+        if (!covered(keys ? A.k_offsets : A.q_offsets, keys ? A.k_lengths : A.q_lengths, A.S, N, (int)token)) return;
         float sum[3] = {0, 0, 0};
-        for (int h = 0; h < H; ++h)
+        for (int h = 0; h < planes; ++h)
             for (int c = 0; c < 3; ++c) sum[c] += part[((int64_t)h * N + token) * 3 + c];
         for (int c = 0; c < 3; ++c) g[token * 3 + c] = sum[c];
         return;
@@ -328,11 +430,7 @@ __global__ __launch_bounds__(SUM_THREADS) void k_dense_bwd_sums(DenseParams A, f
     const int h = b - q_blocks - k_blocks;
     __shared__ double s[SUM_THREADS];
     double sum = 0;
-    for (int seg = 0; seg < A.S; ++seg) {
-        int first, n;
-        segment_range(A.q_offsets, A.q_lengths, seg, A.Nq, first, n);
-        for (int i = threadIdx.x; i < n; i += SUM_THREADS) sum += (double)A.slope_part[(int64_t)(first + i) * Hq + h];
-    }
+    for (int64_t i = threadIdx.x; i < slope_lines; i += SUM_THREADS) sum += (double)A.slope_part[i * Hq + h];
     s[threadIdx.x] = sum;
     __syncthreads();
     for (int o = SUM_THREADS / 2; o; o >>= 1) {
@@ -342,29 +440,71 @@ __global__ __launch_bounds__(SUM_THREADS) void k_dense_bwd_sums(DenseParams A, f
     if (threadIdx.x == 0) gslope[h] = (float)s[0];
 }
 
-// Workgroups of four waves and 128 rows (keys), or of one wave where a segment has no more than 64 of them on average.
+// Sums of the parts' rows, for the covered tokens: a thread for four features.
+template <typename T>
+__global__ __launch_bounds__(SUM_THREADS) void k_dense_bwd_join(Rows out, const float* part, int parts, const int32_t* offsets,
+                                                                const int32_t* lengths, int S, int N, int H, int D) {
+    const int quads = D / 4;
+    const int64_t i = (int64_t)blockIdx.x * SUM_THREADS + threadIdx.x, row = i / quads;
+    if (row >= (int64_t)N * H) return;
+    const int d = (int)(i % quads) * 4, token = (int)(row / H);
+    if (!covered(offsets, lengths, S, N, token)) return;
+    f32x4 sum = {0, 0, 0, 0};
+    for (int p = 0; p < parts; ++p) sum += *reinterpret_cast<const f32x4*>(part + ((int64_t)p * N * H + row) * D + d);
+    char* to = out.row(token, row % H) + d * sizeof(T);
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(to) = sum;
+    else *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
+}
+
+// Workgroups of four waves and 128 rows (keys), or of one wave where a segment has no more than 64 of them on average; and parts of the
+// other side where these are too few to fill the chip.
 struct BwdPlan {
-    int row_waves, key_waves;
+    int row_waves, key_waves, row_parts, key_parts;
     int64_t row_tiles, key_tiles;
 };
+int parts_of(int64_t workgroups, int64_t most) {
+    int64_t parts = workgroups > 0 ? WANT / workgroups : 1;
+    if (parts > most) parts = most;
+    return parts > 64 ? 64 : parts > 1 ? (int)parts : 1;
+}
 BwdPlan bwd_plan(const e2f_dense_args* a) {
     const int group = a->Hq / a->Hk;
-    const int64_t S = a->S;
-    BwdPlan P;
-    P.row_waves = (int64_t)a->Nq * group > 64 * S ? 4 : 1;
+    const int64_t S = a->S, rows = (int64_t)a->Nq * group;
+    BwdPlan P = {1, 1, 1, 1, 0, 0};
+    if (S == 0) return P;
+    P.row_waves = rows > 64 * S ? 4 : 1;
     P.key_waves = a->Nk > 64 * S ? 4 : 1;
-    P.row_tiles = a->Nq && S ? dense_tiles(a->Nq, group, a->S, 32 * P.row_waves) : 0;
-    P.key_tiles = a->Nk && S ? dense_tiles(a->Nk, 1, a->S, 32 * P.key_waves) : 0;
+    P.row_tiles = a->Nq ? dense_tiles(a->Nq, group, a->S, 32 * P.row_waves) : 0;
+    P.key_tiles = a->Nk ? dense_tiles(a->Nk, 1, a->S, 32 * P.key_waves) : 0;
+    P.row_parts = parts_of(P.row_tiles * a->Hk * P.row_waves, a->Nk / S / 256);
+    P.key_parts = parts_of(P.key_tiles * a->Hk * P.key_waves, rows / S / 256);
     return P;
 }
 
 template <typename T, int DP>
 void launch_dp(const DenseParams& A, const BwdPlan& P, hipStream_t st) {
-    const unsigned rows = (unsigned)(P.row_tiles * A.Hk), keys = (unsigned)(P.key_tiles * A.Hk);
-    if (rows && P.row_waves == 4) k_dense_bwd_rows<T, DP, 4><<<rows, 256, 0, st>>>(A);
-    else if (rows) k_dense_bwd_rows<T, DP, 1><<<rows, 64, 0, st>>>(A);
-    if (keys && P.key_waves == 4) k_dense_bwd_keys<T, DP, 4><<<keys, 256, 0, st>>>(A);
-    else if (keys) k_dense_bwd_keys<T, DP, 1><<<keys, 64, 0, st>>>(A);
+    const dim3 rows((unsigned)(P.row_tiles * A.Hk), (unsigned)P.row_parts), keys((unsigned)(P.key_tiles * A.Hk), (unsigned)P.key_parts);
+    const int64_t n = (int64_t)A.Nq * A.Hk * A.group;
+    if (rows.x) {
+        if (P.row_waves == 4) k_dense_bwd_stats<T, DP, 4><<<rows, 256, 0, st>>>(A);
+        else k_dense_bwd_stats<T, DP, 1><<<rows, 64, 0, st>>>(A);
+        if (P.row_parts > 1) k_dense_bwd_join_stats<<<(unsigned)((n + SUM_THREADS - 1) / SUM_THREADS), SUM_THREADS, 0, st>>>(A, P.row_parts);
+        if (P.row_waves == 4) k_dense_bwd_rows<T, DP, 4><<<rows, 256, 0, st>>>(A);
+        else k_dense_bwd_rows<T, DP, 1><<<rows, 64, 0, st>>>(A);
+    }
+    if (keys.x) {
+        if (P.key_waves == 4) k_dense_bwd_keys<T, DP, 4><<<keys, 256, 0, st>>>(A);
+        else k_dense_bwd_keys<T, DP, 1><<<keys, 64, 0, st>>>(A);
+    }
+    auto join = [&](const Rows& out, const float* part, int parts, const int32_t* offsets, const int32_t* lengths, int N, int H) {
+        const int64_t threads = (int64_t)N * H * (A.D / 4);
+        k_dense_bwd_join<T><<<(unsigned)((threads + SUM_THREADS - 1) / SUM_THREADS), SUM_THREADS, 0, st>>>(out, part, parts, offsets, lengths, A.S, N, H, A.D);
+    };
+    if (rows.x && P.row_parts > 1) join(A.out, A.gq_part, P.row_parts, A.q_offsets, A.q_lengths, A.Nq, A.Hk * A.group);
+    if (keys.x && P.key_parts > 1) {
+        join(A.gk, A.gk_part, P.key_parts, A.k_offsets, A.k_lengths, A.Nk, A.Hk);
+        join(A.gv, A.gv_part, P.key_parts, A.k_offsets, A.k_lengths, A.Nk, A.Hk);
+    }
 }
 
 template <typename T>
@@ -375,24 +515,33 @@ void launch(const DenseParams& A, const BwdPlan& P, hipStream_t st) {
     else launch_dp<T, 128>(A, P, st);
 }
 
-// Workspace: statistics of the rows, then what the three sums need (always, so that the size does not depend on what is asked for).
-size_t layout(const e2f_dense_args* a, char* ws, DenseParams* A) {
+// Workspace: statistics of the rows, what the three sums need (always, so that the size does not depend on which are asked for),
+// and the parts' rows.
+size_t layout(const e2f_dense_args* a, const BwdPlan& P, char* ws, DenseParams* A) {
     size_t off = 0;
-    auto take = [&](size_t bytes) {
+    auto take = [&](size_t floats) {
         char* p = ws ? ws + off : nullptr;
-        off += e2f_align_up(bytes);
-        return p;
+        off += e2f_align_up(floats * sizeof(float));
+        return reinterpret_cast<float*>(p);
     };
-    const size_t rows = (size_t)a->Nq * a->Hq;
-    char* stats = take(rows * sizeof(float4));
-    char* slope = a->slope ? take(rows * sizeof(float)) : nullptr;
-    char* qp = a->slope ? take(rows * 3 * sizeof(float)) : nullptr;
-    char* kp = a->slope ? take((size_t)a->Nk * a->Hk * 3 * sizeof(float)) : nullptr;
+    const size_t rows = (size_t)a->Nq * a->Hq, keys = (size_t)a->Nk * a->Hk, rp = P.row_parts, kp = P.key_parts;
+    float* stats = take(rows * 4);
+    float* slope = take(a->slope ? rp * P.row_tiles * a->Hq : 0);
+    float* qp = take(a->slope ? rp * rows * 3 : 0);
+    float* kpos = take(a->slope ? kp * keys * 3 : 0);
+    float* stats_part = take(rp > 1 ? rp * rows * 4 : 0);
+    float* gq = take(rp > 1 ? rp * rows * a->D : 0);
+    float* gk = take(kp > 1 ? kp * keys * a->D : 0);
+    float* gv = take(kp > 1 ? kp * keys * a->D : 0);
     if (A) {
         A->stats = reinterpret_cast<float4*>(stats);
-        A->slope_part = reinterpret_cast<float*>(slope);
-        A->q_pos_part = reinterpret_cast<float*>(qp);
-        A->k_pos_part = reinterpret_cast<float*>(kp);
+        A->slope_part = slope;
+        A->q_pos_part = qp;
+        A->k_pos_part = kpos;
+        A->stats_part = reinterpret_cast<float4*>(stats_part);
+        A->gq_part = gq;
+        A->gk_part = gk;
+        A->gv_part = gv;
     }
     return off;
 }
@@ -402,7 +551,7 @@ size_t layout(const e2f_dense_args* a, char* ws, DenseParams* A) {
 extern "C" {
 
 size_t e2f_dense_attn_backward_workspace_bytes(const e2f_dense_args* a) {
-    return dense_check_sizes(a) == E2F_OK ? layout(a, nullptr, nullptr) : 0;
+    return dense_check_sizes(a) == E2F_OK ? layout(a, bwd_plan(a), nullptr, nullptr) : 0;
 }
 
 e2f_status e2f_dense_attn_backward(const e2f_dense_args* a, const e2f_heads* q, const e2f_heads* k, const e2f_heads* v,
@@ -418,13 +567,14 @@ e2f_status e2f_dense_attn_backward(const e2f_dense_args* a, const e2f_heads* q, 
         (rc = check_result_rows(grad_v, a->dtype, a->Nk, a->Hk, a->D)) != E2F_OK)
         return rc;
     if ((grad_slope || grad_q_pos || grad_k_pos) && !a->slope) return E2F_ERR_INVALID_ARG;
-    const size_t need = layout(a, nullptr, nullptr);
+    const BwdPlan P = bwd_plan(a);
+    const size_t need = layout(a, P, nullptr, nullptr);
     if (need && (!ws || !aligned_ws(ws))) return E2F_ERR_INVALID_ARG;
     if (ws_bytes < need) return E2F_ERR_WORKSPACE_TOO_SMALL;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     DenseParams A;
     dense_fill(A, a, q, k, v);
-    layout(a, static_cast<char*>(ws), &A);
+    layout(a, P, static_cast<char*>(ws), &A);
     A.out = rows_of(grad_q, a->dtype);
     A.go = rows_of(grad_out, a->dtype);
     A.gk = rows_of(grad_k, a->dtype);
@@ -432,7 +582,6 @@ e2f_status e2f_dense_attn_backward(const e2f_dense_args* a, const e2f_heads* q, 
     if (!grad_slope) A.slope_part = nullptr;
     if (!grad_q_pos) A.q_pos_part = nullptr;
     if (!grad_k_pos) A.k_pos_part = nullptr;
-    const BwdPlan P = bwd_plan(a);
     if (P.row_tiles || P.key_tiles) {
         if (a->dtype == E2F_BF16) launch<uint16_t>(A, P, st);
         else launch<float>(A, P, st);
@@ -442,7 +591,7 @@ e2f_status e2f_dense_attn_backward(const e2f_dense_args* a, const e2f_heads* q, 
     const int k_blocks = grad_k_pos && P.key_tiles ? (a->Nk + SUM_THREADS - 1) / SUM_THREADS : 0;
     const int blocks = q_blocks + k_blocks + (grad_slope ? a->Hq : 0);
     if (blocks) {
-        k_dense_bwd_sums<<<blocks, SUM_THREADS, 0, st>>>(A, grad_q_pos, grad_k_pos, grad_slope, q_blocks, k_blocks);
+        k_dense_bwd_sums<<<blocks, SUM_THREADS, 0, st>>>(A, grad_q_pos, grad_k_pos, grad_slope, q_blocks, k_blocks, P.row_parts, P.key_parts, P.row_tiles * P.row_parts);
         E2F_HIP_CHECK(hipGetLastError());
     }
     return E2F_OK;

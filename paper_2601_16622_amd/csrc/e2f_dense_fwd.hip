@@ -19,7 +19,7 @@ struct FwdShape {
 };
 
 template <typename T, int DP, int ROWW, int KEYW>
-__global__ __launch_bounds__(64 * ROWW * KEYW) void k_dense_fwd(DenseParams A) {
+__global__ __launch_bounds__(64 * ROWW * KEYW, 2) void k_dense_fwd(DenseParams A) {
     using F = FwdShape<T, DP, ROWW, KEYW>;
     using M = typename F::M;
     constexpr int BN = F::BN;
@@ -75,7 +75,8 @@ __global__ __launch_bounds__(64 * ROWW * KEYW) void k_dense_fwd(DenseParams A) {
         const int n = min(BN, end - t);
         for (int m = 0; m < n; m += 32) {
             f32x16 p = M::dot(tile.k, m, qf, lane);
-            cap_scores<false>(p, p, A.score, reference_base(top));
+            if constexpr (sizeof(T) == 2) cap_scores_coarse(p, A.score, reference_base(top));
+            else cap_scores<false>(p, p, A.score, reference_base(top));
             if (A.score.biased) bias_scores<BN>(p, x, y, z, slope, tile.place, m + 4 * half);
             if (n - m < 32) {
 #pragma unroll
@@ -147,51 +148,68 @@ __global__ __launch_bounds__(64 * ROWW * KEYW) void k_dense_fwd(DenseParams A) {
     }
 }
 
-// Joins the parts of a row: out = sum_p 2^(top_p - top) part_p / sum_p 2^(top_p - top) sum_p.  A workgroup for a row, its waves
-// take turns at the parts.
-constexpr int JOIN_WAVES = 4;
+// Joins the parts of a row: out = sum_p 2^(top_p - top) part_p / sum_p 2^(top_p - top) sum_p.  A workgroup for a row; its waves
+// share the parts, a lane forms a part's factor, then all lanes walk over the features of the wave's parts, whose loads do
+// not wait for each other.
+constexpr int JOIN_WAVES = 8;
 template <typename T>
 __global__ __launch_bounds__(64 * JOIN_WAVES) void k_dense_join(DenseParams A, int parts) {
-    __shared__ float sums[JOIN_WAVES][128], weight[JOIN_WAVES];
+    __shared__ float sums[JOIN_WAVES][128], weight[JOIN_WAVES], best[JOIN_WAVES];
     const int Hq = A.Hk * A.group, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t row = blockIdx.x, stride = (int64_t)A.Nq * Hq;
     const int query = (int)(row / Hq);
-    int first, n, s = token_segment(A.q_offsets, A.S, query);
+    const int s = token_segment(A.q_offsets, A.S, query);
+    int first, n, k_first, nk;
     segment_range(A.q_offsets, A.q_lengths, s, A.Nq, first, n);
+    segment_range(A.k_offsets, A.k_lengths, s, A.Nk, k_first, nk);
     if (query < first || query >= first + n) return;
+    const int each = (parts + JOIN_WAVES - 1) / JOIN_WAVES, p0 = wave * each, p1 = min(parts, p0 + each);
     float top = -INFINITY;
-    for (int p = lane; p < parts; p += 64) top = fmaxf(top, A.part_sum[(p * stride + row) * 2]);
+    for (int p = p0 + lane; p < p1; p += 64) top = fmaxf(top, A.part_sum[(p * stride + row) * 2]);
 #pragma unroll
     for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if (lane == 0) best[wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < JOIN_WAVES; ++w) top = fmaxf(top, best[w]);
     float a0 = 0, a1 = 0, sum = 0;
-    for (int p = wave; p < parts; p += JOIN_WAVES) {
-        const float t = A.part_sum[(p * stride + row) * 2];
-        if (!(A.part_sum[(p * stride + row) * 2 + 1] != 0.0f)) continue;     // no keys in this part (a NaN counts)
-        const float f = __builtin_amdgcn_exp2f(t - top);
-        const float* part = A.part + (p * stride + row) * A.D;
-        sum += f * A.part_sum[(p * stride + row) * 2 + 1];
-        if (lane < A.D) a0 += f * part[lane];
-        if (lane + 64 < A.D) a1 += f * part[lane + 64];
+    for (int q = p0; q < p1; q += 64) {
+        float f = 0;
+        if (q + lane < p1) {
+            const float* of = A.part_sum + ((q + lane) * stride + row) * 2;
+            // a part without keys has a sum of 0 and left nothing to read
+            f = of[1] != 0.0f ? __builtin_amdgcn_exp2f(of[0] - top) : -1.0f;
+            if (f >= 0.0f || f != f) sum += f * of[1];
+        }
+        const int m = min(64, p1 - q);
+#pragma unroll 8
+        for (int i = 0; i < m; ++i) {
+            const float g = __shfl(f, i);
+            const float* part = A.part + ((q + i) * stride + row) * A.D;
+            const bool in = !(g < 0.0f);
+            const float x0 = in && lane < A.D ? part[lane] : 0.0f, x1 = in && lane + 64 < A.D ? part[lane + 64] : 0.0f;
+            a0 += in ? g * x0 : 0.0f;
+            a1 += in ? g * x1 : 0.0f;
+        }
     }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
     sums[wave][lane] = a0;
     sums[wave][lane + 64] = a1;
     if (lane == 0) weight[wave] = sum;
     __syncthreads();
-    if (wave > 0) return;
-    int k_first, nk;
-    segment_range(A.k_offsets, A.k_lengths, s, A.Nk, k_first, nk);
+    if (threadIdx.x >= (unsigned)A.D) return;
     sum = 0;
+    float a = 0;
 #pragma unroll
-    for (int w = 0; w < JOIN_WAVES; ++w) sum += weight[w];
-    char* out = A.out.row(query, row % Hq);
-    for (int d = lane; d < A.D; d += 64) {
-        float a = 0;
-#pragma unroll
-        for (int w = 0; w < JOIN_WAVES; ++w) a += sums[w][d];
-        a = nk > 0 ? a / sum : 0.0f;
-        if constexpr (sizeof(T) == 4) reinterpret_cast<float*>(out)[d] = a;
-        else reinterpret_cast<uint16_t*>(out)[d] = (uint16_t)pack_bf16(a, 0.0f);
+    for (int w = 0; w < JOIN_WAVES; ++w) {
+        sum += weight[w];
+        a += sums[w][threadIdx.x];
     }
+    a = nk > 0 ? a / sum : 0.0f;
+    char* out = A.out.row(query, row % Hq);
+    if constexpr (sizeof(T) == 4) reinterpret_cast<float*>(out)[threadIdx.x] = a;
+    else reinterpret_cast<uint16_t*>(out)[threadIdx.x] = (uint16_t)pack_bf16(a, 0.0f);
 }
 
 // Which form runs, from the sizes that the host knows.
