@@ -385,16 +385,20 @@ def _feature_type(t, where):
 
 def _heads(t, like, shape, where):
     """[N][H][D] tensor of the type and on the device of `like`, features side by side -> Heads."""
-    _need(t.dtype == like.dtype and t.device == like.device and t.shape == shape and (shape[2] <= 1 or t.stride(2) == 1), where)
-    s = t.stride()
-    return Heads(t.data_ptr(), s[0], s[1])
+    if t.shape != shape or t.dtype != like.dtype or t.device != like.device:
+        _need(False, where)
+    token, head, feature = t.stride()
+    if feature != 1 and shape[2] > 1:
+        _need(False, where)
+    return Heads(t.data_ptr(), token, head)
 
 
 def _plain(t, like, dtype, shape, where):
     """Contiguous tensor of a type and shape on the device of `like` -> its address; None -> None."""
     if t is None:
         return None
-    _need(t.dtype == dtype and t.device == like.device and t.shape == shape and t.is_contiguous(), where)
+    if t.dtype != dtype or t.shape != shape or t.device != like.device or not t.is_contiguous():
+        _need(False, where)
     return t.data_ptr()
 
 
@@ -402,10 +406,18 @@ def _on(device, call, *args):
     """call(*args, stream) with the device current."""
     import torch
     _need(device.type == "cuda", call.__name__)
-    if device.index == torch.cuda.current_device():
-        return call(*args, torch.cuda.current_stream(device).cuda_stream)
-    with torch.cuda.device(device):
-        return call(*args, torch.cuda.current_stream(device).cuda_stream)
+    at = device.index
+    if at == torch.cuda.current_device():
+        return call(*args, _raw_stream(at))
+    with torch.cuda.device(at):
+        return call(*args, _raw_stream(at))
+
+
+def _raw_stream(index):
+    """The current stream's handle; without making a Stream object (2 us of a call's 15) where this torch can."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
 
 
 def _bytes_of(ws, like, where):

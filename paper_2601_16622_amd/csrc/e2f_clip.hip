@@ -52,17 +52,33 @@ __device__ __forceinline__ int tensor_of(const Batch& B, int b) {
     return lo;
 }
 
+// Whole vectors of a chunk, AHEAD of them on their way at once for each thread: body(first element, the vector).
+constexpr int AHEAD = 4;
+template <typename T, class Body>
+__device__ __forceinline__ void vectors(const T* p, int64_t whole, Body body) {
+    constexpr int V = Vec<T>::V;
+    int64_t i = (int64_t)threadIdx.x * V;
+    for (; i + (AHEAD - 1) * THREADS * V < whole; i += AHEAD * THREADS * V) {
+        u32x4 x[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) x[j] = *reinterpret_cast<const Loose<T>*>(p + i + j * THREADS * V);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) body(i + j * THREADS * V, x[j]);
+    }
+    for (; i < whole; i += THREADS * V) body(i, *reinterpret_cast<const Loose<T>*>(p + i));
+}
+
 template <typename T>
 __device__ __forceinline__ double squares(const T* p, int64_t n) {
     constexpr int V = Vec<T>::V;
     double sum = 0;
     const int64_t whole = n / V * V;
-    for (int64_t i = (int64_t)threadIdx.x * V; i < whole; i += THREADS * V) {
+    vectors(p, whole, [&](int64_t, u32x4 x) {
         float f[V];
-        Vec<T>::unpack(*reinterpret_cast<const Loose<T>*>(p + i), f);
+        Vec<T>::unpack(x, f);
 #pragma unroll
         for (int u = 0; u < V; ++u) sum += (double)f[u] * (double)f[u];
-    }
+    });
     for (int64_t i = whole + threadIdx.x; i < n; i += THREADS) {
         float f;
         if constexpr (sizeof(T) == 4) f = p[i]; else f = __uint_as_float((uint32_t)p[i] << 16);
@@ -86,13 +102,13 @@ template <typename T>
 __device__ __forceinline__ void scaled(const T* p, T* q, int64_t n, float factor) {
     constexpr int V = Vec<T>::V;
     const int64_t whole = n / V * V;
-    for (int64_t i = (int64_t)threadIdx.x * V; i < whole; i += THREADS * V) {
+    vectors(p, whole, [&](int64_t i, u32x4 x) {
         float f[V];
-        Vec<T>::unpack(*reinterpret_cast<const Loose<T>*>(p + i), f);
+        Vec<T>::unpack(x, f);
 #pragma unroll
         for (int u = 0; u < V; ++u) f[u] *= factor;
         *reinterpret_cast<Loose<T>*>(q + i) = Vec<T>::pack(f);
-    }
+    });
     for (int64_t i = whole + threadIdx.x; i < n; i += THREADS) {
         if constexpr (sizeof(T) == 4) q[i] = p[i] * factor;
         else q[i] = (uint16_t)pack_bf16(__uint_as_float((uint32_t)p[i] << 16) * factor, 0.0f);
@@ -105,8 +121,7 @@ __device__ __forceinline__ void copied(const T* p, T* q, int64_t n) {
     if (p == q) return;
     constexpr int V = Vec<T>::V;
     const int64_t whole = n / V * V;
-    for (int64_t i = (int64_t)threadIdx.x * V; i < whole; i += THREADS * V)
-        *reinterpret_cast<Loose<T>*>(q + i) = *reinterpret_cast<const Loose<T>*>(p + i);
+    vectors(p, whole, [&](int64_t i, u32x4 x) { *reinterpret_cast<Loose<T>*>(q + i) = x; });
     for (int64_t i = whole + threadIdx.x; i < n; i += THREADS) q[i] = p[i];
 }
 
@@ -118,9 +133,9 @@ __global__ __launch_bounds__(THREADS) void k_clip_scale(Batch B, const double* p
     for (int i = threadIdx.x; i < n_partial; i += THREADS) sum += partial[i];
     sum = block_sum(sum, s);
     const double root = sqrt(sum), ratio = (double)max_norm / (root + 1e-6);
-    const int b = blockIdx.x;
-    if (b == 0 && threadIdx.x == 0 && norm) *norm = (float)root;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && norm) *norm = (float)root;
     if (!B.n) return;
+    const int b = gridDim.x - 1 - blockIdx.x;      // the last chunks first: the pass before has just read them
     const int t = tensor_of(B, b), first = B.first[t];
     const int64_t at = (int64_t)(b - (first & 0x7FFFFFFF)) * B.chunk, n = min(B.chunk, B.count[t] - at);
     const bool clip = ratio < 1.0 && root < (double)INFINITY;   // false for a NaN too

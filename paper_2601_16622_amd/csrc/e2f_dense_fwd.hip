@@ -148,10 +148,39 @@ __global__ __launch_bounds__(64 * ROWW * KEYW, 2) void k_dense_fwd(DenseParams A
     }
 }
 
-// Joins the parts of a row: out = sum_p 2^(top_p - top) part_p / sum_p 2^(top_p - top) sum_p.  A workgroup for a row; its waves
-// share the parts, a lane forms a part's factor, then all lanes walk over the features of the wave's parts, whose loads do
+// Joins the parts of a row: out = sum_p 2^(top_p - top) part_p / sum_p 2^(top_p - top) sum_p.  For a few parts of many rows, a thread
+// for four features of a row: at 2 parts of 80 000 rows of 64 features it moves its 84 MB in TBD us.
+template <typename T>
+__global__ __launch_bounds__(256) void k_dense_join_few(DenseParams A, int parts) {
+    const int Hq = A.Hk * A.group, quads = A.D / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / quads, stride = (int64_t)A.Nq * Hq;
+    if (row >= stride) return;
+    const int d = (int)(i % quads) * 4, query = (int)(row / Hq);
+    const int s = token_segment(A.q_offsets, A.S, query);
+    int first, n, k_first, nk;
+    segment_range(A.q_offsets, A.q_lengths, s, A.Nq, first, n);
+    if (query < first || query >= first + n) return;
+    segment_range(A.k_offsets, A.k_lengths, s, A.Nk, k_first, nk);
+    const f32x2* of = reinterpret_cast<const f32x2*>(A.part_sum) + row;
+    float top = -INFINITY, sum = 0;
+    for (int p = 0; p < parts; ++p) top = fmaxf(top, of[p * stride][0]);
+    f32x4 a = {0, 0, 0, 0};
+    for (int p = 0; p < parts; ++p) {
+        const f32x2 r = of[p * stride];
+        if (!(r[1] != 0.0f)) continue;       // no keys in this part, which then left nothing to read
+        const float f = __builtin_amdgcn_exp2f(r[0] - top);
+        sum += f * r[1];
+        a += f * *reinterpret_cast<const f32x4*>(A.part + (p * stride + row) * A.D + d);
+    }
+    a = nk > 0 ? a / sum : f32x4{0, 0, 0, 0};
+    char* to = A.out.row(query, row % Hq) + d * sizeof(T);
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(to) = a;
+    else *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
+}
+
+// For many parts of a few rows, a workgroup for a row; its waves share the parts, a lane forms a part's factor, then all lanes walk over the features of the wave's parts, whose loads do
 // not wait for each other.
-constexpr int JOIN_WAVES = 8;
+constexpr int JOIN_WAVES = 16, JOIN_FEW = 8;
 template <typename T>
 __global__ __launch_bounds__(64 * JOIN_WAVES) void k_dense_join(DenseParams A, int parts) {
     __shared__ float sums[JOIN_WAVES][128], weight[JOIN_WAVES], best[JOIN_WAVES];
@@ -182,7 +211,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_dense_join(DenseParams A, i
             if (f >= 0.0f || f != f) sum += f * of[1];
         }
         const int m = min(64, p1 - q);
-#pragma unroll 8
+#pragma unroll 16
         for (int i = 0; i < m; ++i) {
             const float g = __shfl(f, i);
             const float* part = A.part + ((q + i) * stride + row) * A.D;
@@ -226,11 +255,21 @@ FwdPlan fwd_plan(const e2f_dense_args* a) {
         P.keyw = a->Nk > 128 * S ? 4 : 1;
     }
     P.tiles = dense_tiles(a->Nq, group, a->S, 32 * P.roww);
-    const int64_t have = P.tiles * a->Hk, want = 512, most = a->Nk / S / (64 * P.keyw);
-    int64_t parts = have > 0 ? want / have : 1;
-    if (parts > most) parts = most;
-    if (parts > 1024) parts = 1024;
-    if (parts > 1) P.parts = (int)parts;
+    if (P.tiles == 0) return P;
+    const int64_t blocks = P.tiles * a->Hk, keys = a->Nk / S;
+    if (P.roww == 4) {
+        // two workgroups to a compute unit; a round over 10 000 keys with 64 (128) features takes 354 (524) us in bf16, 900 (1 500) in
+        // fp32.  Two parts instead of one: 10 000 atoms, 8 heads, 632 workgroups 708 -> 587 us; 4 000 atoms in fp32, 264 workgroups,
+        // 359 -> 367, and stays in one
+        const double per_key = a->dtype == E2F_BF16 ? 0.018 + 0.00027 * a->D : 0.03 + 0.00094 * a->D;
+        P.parts = best_parts(blocks, 512, keys * per_key, rows * a->Hk * (a->D * 8.0) / 4.5e6, keys / 256);
+    } else {
+        // a few rows: their keys over 2048 waves, each with two tiles at least
+        int64_t parts = 2048 / (blocks * P.keyw);
+        const int64_t most = keys / (64 * P.keyw);
+        if (parts > most) parts = most;
+        P.parts = parts > 1 ? (int)(parts < 1024 ? parts : 1024) : 1;
+    }
     return P;
 }
 
@@ -240,7 +279,9 @@ void launch_dp(const DenseParams& A, const FwdPlan& P, hipStream_t st) {
     if (P.roww == 4) k_dense_fwd<T, DP, 4, 1><<<grid, 256, 0, st>>>(A);
     else if (P.keyw == 4) k_dense_fwd<T, DP, 1, 4><<<grid, 256, 0, st>>>(A);
     else k_dense_fwd<T, DP, 1, 1><<<grid, 64, 0, st>>>(A);
-    if (P.parts > 1) k_dense_join<T><<<(unsigned)((int64_t)A.Nq * A.Hk * A.group), 64 * JOIN_WAVES, 0, st>>>(A, P.parts);
+    const int64_t rows = (int64_t)A.Nq * A.Hk * A.group;
+    if (P.parts > JOIN_FEW) k_dense_join<T><<<(unsigned)rows, 64 * JOIN_WAVES, 0, st>>>(A, P.parts);
+    else if (P.parts > 1) k_dense_join_few<T><<<(unsigned)((rows * (A.D / 4) + 255) / 256), 256, 0, st>>>(A, P.parts);
 }
 
 template <typename T>

@@ -187,19 +187,25 @@ __global__ __launch_bounds__(THREADS) void k_qk_bwd(QkParams A) {
     }
 }
 
-// Sums of the partial rows: a workgroup for 16 columns, 16 threads down each.
-__global__ __launch_bounds__(THREADS) void k_qk_weight_sums(const float* partial, int lines, int D, float* gq, float* gk) {
-    __shared__ double s[16][17];
+// Sums of the partial rows: a workgroup for 16 columns, 64 threads down each.
+constexpr int SUM_THREADS = 1024;
+__global__ __launch_bounds__(SUM_THREADS) void k_qk_weight_sums(const float* partial, int lines, int D, float* gq, float* gk) {
+    constexpr int DOWN = SUM_THREADS / 16;
+    __shared__ double s[DOWN][16];
     const int col = blockIdx.x * 16 + threadIdx.x % 16, down = threadIdx.x / 16;
     double sum = 0;
-    if (col < 2 * D)
-        for (int l = down; l < lines; l += 16) sum += (double)partial[(int64_t)l * 2 * D + col];
+    if (col < 2 * D) {
+#pragma unroll 4
+        for (int l = down; l < lines; l += DOWN) sum += (double)partial[(int64_t)l * 2 * D + col];
+    }
     s[down][threadIdx.x % 16] = sum;
-    __syncthreads();
+    for (int o = DOWN / 2; o; o >>= 1) {
+        __syncthreads();
+        if (down < o) s[down][threadIdx.x % 16] += s[down + o][threadIdx.x % 16];
+    }
     if (down == 0 && col < 2 * D) {
-        for (int d = 1; d < 16; ++d) sum += s[d][threadIdx.x];
         float* g = col < D ? gq : gk;
-        if (g) g[col < D ? col : col - D] = (float)sum;
+        if (g) g[col < D ? col : col - D] = (float)s[0][threadIdx.x];
     }
 }
 
@@ -361,7 +367,7 @@ e2f_status e2f_qk_norm_rotate_backward(const e2f_qk_args* a, const e2f_heads* q,
         E2F_HIP_CHECK(hipGetLastError());
     }
     if (sums) {   // without rows: zeros
-        k_qk_weight_sums<<<(2 * a->D + 15) / 16, THREADS, 0, st>>>(static_cast<float*>(ws), (int)(g.x * g.y), a->D,
+        k_qk_weight_sums<<<(2 * a->D + 15) / 16, SUM_THREADS, 0, st>>>(static_cast<float*>(ws), (int)(g.x * g.y), a->D,
                                                                   grad_weight_q, grad_weight_k);
         E2F_HIP_CHECK(hipGetLastError());
     }
