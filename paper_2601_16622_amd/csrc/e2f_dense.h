@@ -35,7 +35,7 @@ struct DenseParams {
     float scale;
     DenseScore score;
     float *part, *part_sum;        // forward with split keys: [splits][Nq][Hq][D] sums over a part's keys, [splits][Nq][Hq][2] reference, sum
-    float4* stats;                 // backward: [Nq][Hq] softmax reference, 1 / sum, delta
+    float4* stats;                 // backward: [Nq][Hq] softmax reference, 1 / sum, delta, reference + log2(sum)
     // of the parts of a backward pass: [parts] of [row tiles][Hq], [Hq][Nq][3], [Hk][Nk][3], [Nq][Hq], [Nq][Hq][D], [Nk][Hk][D]
     float *slope_part, *q_pos_part, *k_pos_part;
     float4* stats_part;
@@ -85,7 +85,7 @@ __device__ __forceinline__ int token_segment(const int32_t* offsets, int S, int 
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
 
 // Matrix instructions and operands of the two feature types.  DP: D rounded up to 32, zero beyond D.  A tile is BN rows of
-// features in LDS, LD elements from row to row.
+// features in LDS, LD elements from row to row, a row's 16-byte pieces in the order piece(row, .).
 template <typename T, int DP>
 struct Mma;
 
@@ -93,7 +93,10 @@ struct Mma;
 template <int DP>
 struct Mma<uint16_t, DP> {
     using T = uint16_t;
-    static constexpr int STEPS = DP / 16, LD = DP + 8;
+    // Rows are 16 banks of 64 apart (modulo 64), so that the transposed reads of 4 rows x 32 features meet no bank twice, and pieces
+    // are exchanged within groups of four by the row, so that the reads of one piece of 8 rows do not either.
+    static constexpr int STEPS = DP / 16, LD = DP == 64 ? 96 : DP == 128 ? 160 : DP;
+    static __device__ __forceinline__ int piece(int row, int i) { return i ^ (row >> 2 & 3); }
     // a row of features as an operand, for products over the features
     struct Frag {
         bf16x8 x[STEPS];
@@ -110,10 +113,11 @@ struct Mma<uint16_t, DP> {
     // A B^T over the features: A 32 rows of a tile
     static __device__ __forceinline__ f32x16 dot(const T* tile, int row0, const Frag& b, int lane) {
         f32x16 acc = {};
-        const T* p = tile + (row0 + (lane & 31)) * LD + 8 * (lane >> 5);
+        const T* row = tile + (row0 + (lane & 31)) * LD;
+        const T* p[2] = {row + 8 * piece(lane, lane >> 5), row + 8 * piece(lane, 2 + (lane >> 5))};      // row0: a multiple of 32
 #pragma unroll
         for (int c = 0; c < STEPS; ++c)
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(p + 16 * c), b.x[c], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(p[c & 1] + 32 * (c >> 1)), b.x[c], acc, 0, 0, 0);
         return acc;
     }
     // weights of 32 tile rows as an operand of products over those rows
@@ -131,18 +135,32 @@ struct Mma<uint16_t, DP> {
         }
         return w;
     }
+    static constexpr int WEIGHT_VECTORS = 2;      // 16-byte pieces of a lane's weights
+    static __device__ __forceinline__ void put(u32x4* to, const Weights& w) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) to[64 * c] = __builtin_bit_cast(u32x4, w.x[c]);
+    }
+    static __device__ __forceinline__ Weights get(const u32x4* from) {
+        Weights w;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) w.x[c] = __builtin_bit_cast(bf16x8, from[64 * c]);
+        return w;
+    }
     // acc[dt] += (features 32 dt .. of the tile, transposed) W over the 32 tile rows from row0.  ds_read_b64_tr_b16 turns 4 rows of 16
     // features in each 16 lanes: lane 4 r + c of them addresses features 4 c .. of row r, lane i gets feature i of the four rows.
-    static __device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const T* tile, int row0, const Weights& w, int lane) {
+    template <int NT>
+    static __device__ __forceinline__ void accumulate(f32x16 (&acc)[NT], const T* tile, int row0, const Weights& w, int lane) {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4* lds4;
-        const T* p = tile + (row0 + 4 * (lane >> 5) + ((lane >> 2) & 3)) * LD + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+        const int half = lane >> 5, i = (lane >> 4 & 1) * 2 + (lane >> 1 & 1);      // rows 4 half .. and 8 + 4 half ..: pieces by half and 2 + half
+        const T* row = tile + (row0 + 4 * half + (lane >> 2 & 3)) * LD + 4 * (lane & 1);
+        const T *p = row + 8 * (i ^ half), *q = row + 8 * LD + 8 * (i ^ (2 + half));
 #pragma unroll
-        for (int dt = 0; dt < DP / 32; ++dt)
+        for (int dt = 0; dt < NT; ++dt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + dt * 32 + 16 * c * LD));
-                const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + dt * 32 + (16 * c + 8) * LD));
+                const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(q + dt * 32 + 16 * c * LD));
                 const auto ab = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
                 acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ab), w.x[c], acc[dt], 0, 0, 0);
             }
@@ -155,6 +173,7 @@ template <int DP>
 struct Mma<float, DP> {
     using T = float;
     static constexpr int LD = DP + 8, H = DP / 2;
+    static __device__ __forceinline__ int piece(int, int i) { return i; }
     struct Frag {
         float x[H];
     };
@@ -183,10 +202,29 @@ struct Mma<float, DP> {
         f32x16 x;
     };
     static __device__ __forceinline__ Weights weights(const f32x16& p) { return Weights{p}; }
-    static __device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const T* tile, int row0, const Weights& w, int lane) {
+    static constexpr int WEIGHT_VECTORS = 4;
+    static __device__ __forceinline__ void put(u32x4* to, const Weights& w) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const f32x4 x = {w.x[4 * c], w.x[4 * c + 1], w.x[4 * c + 2], w.x[4 * c + 3]};
+            to[64 * c] = __builtin_bit_cast(u32x4, x);
+        }
+    }
+    static __device__ __forceinline__ Weights get(const u32x4* from) {
+        Weights w;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const f32x4 x = __builtin_bit_cast(f32x4, from[64 * c]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w.x[4 * c + e] = x[e];
+        }
+        return w;
+    }
+    template <int NT>
+    static __device__ __forceinline__ void accumulate(f32x16 (&acc)[NT], const T* tile, int row0, const Weights& w, int lane) {
         const T* p = tile + (row0 + 4 * (lane >> 5)) * LD + (lane & 31);
 #pragma unroll
-        for (int dt = 0; dt < DP / 32; ++dt)
+        for (int dt = 0; dt < NT; ++dt)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(p[(8 * (i / 4) + i % 4) * LD + dt * 32], w.x[i], acc[dt], 0, 0, 0);
@@ -213,8 +251,8 @@ struct Transfer {
     __device__ __forceinline__ void store(int tid, T* tile) const {
 #pragma unroll
         for (int j = 0; j < EACH; ++j) {
-            const int i = tid + j * THREADS;
-            *reinterpret_cast<u32x4*>(tile + i / VECS * M::LD + i % VECS * V) = x[j];
+            const int i = tid + j * THREADS, r = i / VECS;
+            *reinterpret_cast<u32x4*>(tile + r * M::LD + M::piece(r, i % VECS) * V) = x[j];
         }
     }
 };
@@ -255,46 +293,33 @@ __device__ __forceinline__ void tile_sync() {
 // error 8e-8; scores are rarely near their cap), beyond that 1 - 2 / (1 + e^2x), whose absolute error of 1e-7 is then a relative one.
 // Which form an element gets goes by the element alone, so that a row's result does not depend on the rows beside it; the
 // vote only leaves the second form out where no element of the wave needs it.
-template <bool SLACK>
-__device__ __forceinline__ void cap_scores(f32x16& p, f32x16& slack, const DenseScore& A, float base) {
-    if (!A.capped) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) p[i] = p[i] * A.in - base;
-        if (SLACK) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) slack[i] = 1.0f;
-        }
-        return;
-    }
-    float far = 0.0f;
+// The largest argument's size of a lane; beyond 1 in any lane of the wave (`__any`), FAR is asked for.
+__device__ __forceinline__ float cap_arguments(f32x16& p, const DenseScore& A, float far) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         p[i] *= A.in;
         far = fmaxf(far, fabsf(p[i]));
     }
-    auto polynomial = [&](float x) {
-        const float y = x * x;
+    return far;
+}
+// p: arguments -> scores minus base.
+template <bool SLACK, bool FAR>
+__device__ __forceinline__ void cap_values(f32x16& p, f32x16& slack, const DenseScore& A, float base) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float x = p[i], y = x * x;
         float t = A.c[7];
 #pragma unroll
         for (int k = 6; k >= 0; --k) t = t * y + A.c[k];
-        return t;
-    };
-    auto near = [&](int i) {
-        const float x = p[i], t = polynomial(x);
         if (SLACK) {
             const float v = x * t;
             slack[i] = 1.0f - v * A.inv_out2 * v;
+            p[i] = v - base;
+        } else {
+            p[i] = x * t - base;
         }
-        p[i] = x * t - base;
-    };
-    if (!__any(far > 1.0f)) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) near(i);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float x = p[i], r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f * LOG2E)));
-            near(i);
+        if (FAR) {
+            const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f * LOG2E)));
             if (fabsf(x) > 1.0f) {
                 if (SLACK) slack[i] = 4.0f * r * (1.0f - r);       // 1 - (1 - 2 r)^2
                 p[i] = (1.0f - 2.0f * r) * A.out - base;
@@ -302,13 +327,29 @@ __device__ __forceinline__ void cap_scores(f32x16& p, f32x16& slack, const Dense
         }
     }
 }
+__device__ __forceinline__ void plain_scores(f32x16& p, const DenseScore& A, float base) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p[i] = p[i] * A.in - base;
+}
+template <bool SLACK>
+__device__ __forceinline__ void cap_scores(f32x16& p, f32x16& slack, const DenseScore& A, float base) {
+    if (!A.capped) {
+        plain_scores(p, A, base);
+        if (SLACK) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) slack[i] = 1.0f;
+        }
+        return;
+    }
+    if (!__any(cap_arguments(p, A, 0.0f) > 1.0f)) cap_values<SLACK, false>(p, slack, A, base);
+    else cap_values<SLACK, true>(p, slack, A, base);
+}
 
 // The same with tanh x = 1 - 2 / (1 + e^2x) everywhere: 7 issue slots an element (the exponential and the reciprocal take two each)
 // where the polynomial and its vote take 11.  Its absolute error, 2^-23 of the cap, is for results in bf16 alone.
 __device__ __forceinline__ void cap_scores_coarse(f32x16& p, const DenseScore& A, float base) {
     if (!A.capped) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) p[i] = p[i] * A.in - base;
+        plain_scores(p, A, base);
         return;
     }
     const float in = A.in * (2.0f * LOG2E), out = -2.0f * A.out, over = A.out - base;
@@ -351,13 +392,14 @@ __device__ __forceinline__ void bias_scores(f32x16& p, float x, float y, float z
 }
 
 // 32 x 32 features of a wave's accumulators, transposed: lane l holds row l % 32, features 8 (i/4) + 4 (l/32) + i % 4.
+// The first of the features is d0 of the row's D.
 template <typename T, int DP>
-__device__ __forceinline__ void store_row(char* row, const f32x16 (&acc)[DP / 32], float factor, int D, int half) {
+__device__ __forceinline__ void store_row(char* row, const f32x16 (&acc)[DP / 32], float factor, int D, int half, int d0 = 0) {
 #pragma unroll
     for (int dt = 0; dt < DP / 32; ++dt)
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            const int d = dt * 32 + 8 * b + 4 * half;
+            const int d = d0 + dt * 32 + 8 * b + 4 * half;
             if (d >= D) continue;
             f32x4 x;
 #pragma unroll

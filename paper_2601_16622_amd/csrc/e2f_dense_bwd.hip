@@ -6,17 +6,14 @@
 // dk and dv.  Each sum is formed by the workgroup that owns its row or key, so no atomics are needed; where these are too few to
 // fill the chip the other side is cut into parts, whose sums are joined in their order.  delta comes from the binary32 products and weights (not from the rounded result of the forward pass):
 // the gradients of slope and places are binary32 and keep their precision.
+#include <type_traits>
+
 #include "e2f_dense_api.h"
 
 namespace {
 
 using namespace e2f;
 
-#ifndef WANT
-#define WANT 4096
-#define RMINF (DP <= 96 || sizeof(T) == 2 ? 2 : 1)
-#define KMINF (DP * sizeof(T) <= 128 ? 2 : 1)
-#endif
 constexpr int SUM_THREADS = 256;
 
 // A distance and its reciprocal.  d^2 is kept from 0, so that a pair at one place has a finite reciprocal that the components of
@@ -27,16 +24,17 @@ __device__ __forceinline__ void distance(float dx, float dy, float dz, float& d,
     d = d2 * inv;
 }
 
-// A workgroup's 32 ROWW rows of a (segment, key head), its part of the segment's keys (blockIdx.y), and the walk over them.
-template <typename T, int DP, int ROWW>
+// A workgroup's 32 ROWW rows of a (segment, key head), its part of the segment's keys (blockIdx.y), and the walk over them.  SHARE
+// waves to a group of 32 rows: they take 32 keys of a tile each.
+template <typename T, int DP, int ROWW, int SHARE>
 struct RowWalk {
     using M = Mma<T, DP>;
-    static constexpr int BN = ROWW > 1 && sizeof(T) == 2 ? 64 : 32, BM = 32 * ROWW, THREADS = 64 * ROWW;
+    static constexpr int BN = SHARE > 1 ? 32 * SHARE : ROWW > 1 && sizeof(T) == 2 ? 64 : 32, BM = 32 * ROWW, THREADS = 64 * ROWW * SHARE;
     struct Tile {
         T k[BN * M::LD], v[BN * M::LD];
         float place[3 * BN];
     };
-    int lane, half, head_k, k0, begin, end, query, head, first_head;
+    int lane, half, group, share, head_k, k0, begin, end, query, head, first_head;
     int64_t at;            // of the row among [Nq][Hq]
     bool any, valid, busy;
     float x, y, z, slope;
@@ -45,7 +43,8 @@ struct RowWalk {
     __device__ __forceinline__ RowWalk(const DenseParams& A) {
         lane = threadIdx.x & 63;
         half = lane >> 5;
-        const int wave = threadIdx.x >> 6;
+        group = (threadIdx.x >> 6) % ROWW;
+        share = (threadIdx.x >> 6) / ROWW;
         head_k = blockIdx.x % A.Hk;
         const int64_t tile = blockIdx.x / A.Hk;
         const int s = segment_of(A.q_offsets, A.S, A.Nq, A.group, BM, tile);
@@ -56,9 +55,9 @@ struct RowWalk {
         any = row0 >= 0 && row0 < rows;
         if (!any) return;
         first_head = (int)(row0 % A.group);
-        const int64_t row = row0 + wave * 32 + (lane & 31);
+        const int64_t row = row0 + group * 32 + (lane & 31);
         valid = row < rows;
-        busy = row0 + wave * 32 < rows;
+        busy = row0 + group * 32 < rows;
         const int in_segment = valid ? A.over_group((uint32_t)row) : 0;
         query = q0 + in_segment;
         head = head_k * A.group + (valid ? (int)row - in_segment * A.group : 0);
@@ -76,7 +75,7 @@ struct RowWalk {
             slope = A.slope[head];
         }
     }
-    // body(first row of 32 keys in the tile, how many of them count)
+    // body(first row of 32 keys in the tile, how many of them count); with SHARE, body(whether the wave's rows count, ...) for each wave
     template <class Body>
     __device__ __forceinline__ void walk(const DenseParams& A, Tile& tile, Body body) {
         const int tid = threadIdx.x;
@@ -90,15 +89,19 @@ struct RowWalk {
         };
         if (begin < end) fetch(begin);
         for (int t = begin; t < end; t += BN) {
-            tile_sync<(ROWW > 1)>();
+            __syncthreads();
             tk.store(tid, tile.k);
             tv.store(tid, tile.v);
             if (A.score.biased) tp.store(tid, tile.place);
-            tile_sync<(ROWW > 1)>();
+            __syncthreads();
             if (t + BN < end) fetch(t + BN);
-            if (!busy) continue;
             const int n = min(BN, end - t);
-            for (int m = 0; m < n; m += 32) body(m, n - m);
+            if constexpr (SHARE > 1) {
+                body(32 * share, n - 32 * share);
+            } else {
+                if (!busy) continue;
+                for (int m = 0; m < n; m += 32) body(m, n - m);
+            }
         }
     }
     // keys behind the end: weight 0
@@ -113,7 +116,7 @@ struct RowWalk {
 // Softmax statistics of the rows: reference, sum, sum of p dp.  With parts of the keys each leaves its own, [parts][Nq][Hq].
 template <typename T, int DP, int ROWW>
 __global__ __launch_bounds__(64 * ROWW, 2) void k_dense_bwd_stats(DenseParams A) {
-    using R = RowWalk<T, DP, ROWW>;
+    using R = RowWalk<T, DP, ROWW, 1>;
     using M = typename R::M;
     __shared__ __align__(16) typename R::Tile tile;
     R w(A);
@@ -145,7 +148,7 @@ __global__ __launch_bounds__(64 * ROWW, 2) void k_dense_bwd_stats(DenseParams A)
     if (!w.valid || w.half) return;
     if (gridDim.y == 1) {
         const float inv = w.begin < w.end ? 1.0f / sum : 0.0f;
-        A.stats[w.at] = make_float4(top, inv, delta * inv, 0.0f);
+        A.stats[w.at] = make_float4(top, inv, delta * inv, top - __builtin_amdgcn_logf(inv));
     } else {
         A.stats_part[(int64_t)blockIdx.y * A.Nq * (A.Hk * A.group) + w.at] = make_float4(top, sum, delta, 0.0f);
     }
@@ -164,29 +167,32 @@ __global__ __launch_bounds__(SUM_THREADS) void k_dense_bwd_join_stats(DenseParam
         delta += f * s.z;
     }
     const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;      // no keys: no weights
-    A.stats[row] = make_float4(top, inv, delta * inv, 0.0f);
+    A.stats[row] = make_float4(top, inv, delta * inv, top - __builtin_amdgcn_logf(inv));
 }
 
-// dq and a row's shares of the gradients of slope and place, from the statistics.
-template <typename T, int DP, int ROWW>
-__global__ __launch_bounds__(64 * ROWW, RMINF) void k_dense_bwd_rows(DenseParams A) {
-    using R = RowWalk<T, DP, ROWW>;
+// dq and a row's shares of the gradients of slope and place, from the statistics.  SHARE waves to a group of rows pass each other the
+// weights and keep the sums of DP / SHARE features each, as in the kernel over keys.
+template <typename T, int DP, int ROWW, int SHARE>
+__global__ __launch_bounds__(64 * ROWW * SHARE, DP * sizeof(T) / SHARE <= 256 ? 2 : 1) void k_dense_bwd_rows(DenseParams A) {
+    using R = RowWalk<T, DP, ROWW, SHARE>;
     using M = typename R::M;
-    constexpr int BN = R::BN;
+    constexpr int BN = R::BN, NT = DP / SHARE / 32;
     __shared__ __align__(16) typename R::Tile tile;
+    __shared__ __align__(16) u32x4 passed[SHARE > 1 ? ROWW * SHARE : 1][SHARE > 1 ? M::WEIGHT_VECTORS * 64 : 1];
     R w(A);
+    const int Hq = A.Hk * A.group;
+    float* slopes = A.slope_part ? A.slope_part + ((int64_t)blockIdx.y * (gridDim.x / A.Hk) + blockIdx.x / A.Hk) * Hq + w.head_k * A.group : nullptr;
     if (!w.any) {
-        if (A.slope_part)
-            for (int g = threadIdx.x; g < A.group; g += R::THREADS)
-                A.slope_part[((int64_t)blockIdx.y * (gridDim.x / A.Hk) + blockIdx.x / A.Hk) * (A.Hk * A.group) + w.head_k * A.group + g] = 0.0f;
+        if (slopes)
+            for (int g = threadIdx.x; g < A.group; g += R::THREADS) slopes[g] = 0.0f;
         return;
     }
     const float4 st = A.stats[w.at];
     const float top = st.x, inv = st.y, delta = st.z, slope2 = w.slope * LOG2E;
     // weights stay without 1 / sum: a row's sums get it at the end
     float dslope = 0, gx = 0, gy = 0, gz = 0;
-    f32x16 acc[DP / 32] = {};
-    w.walk(A, tile, [&](int m, int n) {
+    f32x16 acc[NT] = {};
+    auto weigh = [&](int m, int n) {
         f32x16 p = M::dot(tile.k, m, w.qf, w.lane), slack;
         const f32x16 dp = M::dot(tile.v, m, w.gf, w.lane);
         cap_scores<true>(p, slack, A.score, top);
@@ -224,31 +230,62 @@ __global__ __launch_bounds__(64 * ROWW, RMINF) void k_dense_bwd_rows(DenseParams
 #pragma unroll
             for (int i = 0; i < 16; ++i) p[i] *= slack[i];
         }
-        M::accumulate(acc, tile.k, m, M::weights(p), w.lane);
-    });
+        return M::weights(p);
+    };
+    if constexpr (SHARE == 1) {
+        w.walk(A, tile, [&](int m, int n) { M::accumulate(acc, tile.k, m, weigh(m, n), w.lane); });
+    } else {
+        w.walk(A, tile, [&](int m, int n) {
+            if (w.busy) M::put(&passed[w.share * ROWW + w.group][w.lane], weigh(m, n));
+            __syncthreads();
+            if (w.busy) {
+#pragma unroll
+                for (int u = 0; u < SHARE; ++u)
+                    M::accumulate(acc, tile.k + w.share * NT * 32, 32 * u, M::get(&passed[u * ROWW + w.group][w.lane]), w.lane);
+            }
+        });
+    }
     dslope += other_half(dslope);
     gx += other_half(gx);
     gy += other_half(gy);
     gz += other_half(gz);
-    if (A.slope_part) {
+    float* sums = reinterpret_cast<float*>(&tile);      // [SHARE][4][BM]
+    static_assert(sizeof(tile) >= SHARE * 4 * R::BM * 4, "room for the rows' sums");
+    if (SHARE > 1 || slopes) {
+        __syncthreads();
+        if (!w.half) {
+            float* to = sums + w.share * 4 * R::BM + w.group * 32 + w.lane;
+            to[0] = w.valid ? -dslope * inv : 0.0f;
+            to[R::BM] = gx;
+            to[2 * R::BM] = gy;
+            to[3 * R::BM] = gz;
+        }
+        __syncthreads();
+    }
+    if (SHARE > 1 && w.share == 0 && !w.half) {
+#pragma unroll
+        for (int u = 1; u < SHARE; ++u) {
+            const float* from = sums + u * 4 * R::BM + w.group * 32 + w.lane;
+            gx += from[R::BM];
+            gy += from[2 * R::BM];
+            gz += from[3 * R::BM];
+        }
+    }
+    if (slopes) {
         // over the workgroup's rows, for each head of the group, in their order
-        __syncthreads();
-        float* rows = reinterpret_cast<float*>(&tile);
-        if (!w.half) rows[threadIdx.x / 64 * 32 + w.lane] = w.valid ? -dslope * inv : 0.0f;
-        __syncthreads();
-        const int first = w.first_head;       // of row 0 of the workgroup
         for (int g = threadIdx.x; g < A.group; g += R::THREADS) {
             float sum = 0;
-            for (int r = g >= first ? g - first : g - first + A.group; r < R::BM; r += A.group) sum += rows[r];
-            A.slope_part[((int64_t)blockIdx.y * (gridDim.x / A.Hk) + blockIdx.x / A.Hk) * (A.Hk * A.group) + w.head_k * A.group + g] = sum;
+            for (int u = 0; u < SHARE; ++u)
+                for (int r = g >= w.first_head ? g - w.first_head : g - w.first_head + A.group; r < R::BM; r += A.group) sum += sums[u * 4 * R::BM + r];
+            slopes[g] = sum;
         }
     }
     if (!w.valid) return;
-    const int Hq = A.Hk * A.group;
     const int64_t at = (int64_t)blockIdx.y * A.Nq * Hq + w.at;
-    if (gridDim.y == 1) store_row<T, DP>(A.out.row(w.query, w.head), acc, A.scale * inv, A.D, w.half);
-    else store_row<float, DP>(reinterpret_cast<char*>(A.gq_part + at * A.D), acc, A.scale * inv, A.D, w.half);
-    if (w.half) return;
+    const int d0 = w.share * NT * 32;
+    if (gridDim.y == 1) store_row<T, NT * 32>(A.out.row(w.query, w.head), acc, A.scale * inv, A.D, w.half, d0);
+    else store_row<float, NT * 32>(reinterpret_cast<char*>(A.gq_part + at * A.D), acc, A.scale * inv, A.D, w.half, d0);
+    if (w.half || w.share) return;
     if (A.q_pos_part) {
         float* g = A.q_pos_part + (((int64_t)blockIdx.y * Hq + w.head) * A.Nq + w.query) * 3;
         g[0] = -w.slope * inv * gx;
@@ -257,17 +294,23 @@ __global__ __launch_bounds__(64 * ROWW, RMINF) void k_dense_bwd_rows(DenseParams
     }
 }
 
-// What the kernel over keys needs of a row, as lines of BN in LDS.
-enum { ROW_X, ROW_Y, ROW_Z, ROW_SLOPE, ROW_TOP, ROW_INV, ROW_DELTA, ROW_LINES };
+// What the kernel over keys needs of a row, as lines of BN in LDS: place, slope in base-2 units, and with lse = reference + log2(sum) the
+// weight is one exponential (the rounding of lse, 2^-24 of it, scales a row's weights alike).
+enum { ROW_X, ROW_Y, ROW_Z, ROW_SLOPE, ROW_LSE, ROW_DELTA, ROW_LINES };
 
-template <typename T, int DP, int ROWW>
-__global__ __launch_bounds__(64 * ROWW, KMINF) void k_dense_bwd_keys(DenseParams A) {
+// CAP, BIAS: what the scores have.  KEYW groups of 32 keys a workgroup, SHARE waves to a group: they take a block of 32 rows each of a
+// tile, pass each other the weights through LDS and keep the sums of DP / SHARE features each.  With 128 features one wave's operands and sums
+// take more registers than leave room for a second wave on its SIMD.
+template <typename T, int DP, int KEYW, int SHARE, bool CAP, bool BIAS>
+__global__ __launch_bounds__(64 * KEYW * SHARE, 2) void k_dense_bwd_keys(DenseParams A) {
     using M = Mma<T, DP>;
-    constexpr int BN = ROWW > 1 && sizeof(T) == 2 ? 64 : 32, BM = 32 * ROWW, THREADS = 64 * ROWW;
+    constexpr int BN = SHARE > 1 ? 32 * SHARE : KEYW > 1 && sizeof(T) == 2 ? 64 : 32, BM = 32 * KEYW, THREADS = 64 * KEYW * SHARE;
+    constexpr int NT = DP / SHARE / 32;
     __shared__ __align__(16) T qs[BN * M::LD];
     __shared__ __align__(16) T gs[BN * M::LD];
     __shared__ __align__(16) float par[ROW_LINES][BN];
-    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = tid >> 6;
+    __shared__ __align__(16) u32x4 passed[SHARE > 1 ? KEYW * SHARE : 1][2][SHARE > 1 ? M::WEIGHT_VECTORS * 64 : 1];
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = (tid >> 6) % KEYW, share = (tid >> 6) / KEYW;
     const int head_k = blockIdx.x % A.Hk, Hq = A.Hk * A.group;
     const int64_t tile = blockIdx.x / A.Hk;
     const int s = segment_of(A.k_offsets, A.S, A.Nk, 1, BM, tile);
@@ -284,7 +327,7 @@ __global__ __launch_bounds__(64 * ROWW, KMINF) void k_dense_bwd_keys(DenseParams
     M::load(kf, A.k.row(key, head_k), A.D, valid, half);
     M::load(vf, A.v.row(key, head_k), A.D, valid, half);
     float x = 0, y = 0, z = 0;
-    if (A.score.biased) {
+    if (BIAS) {
         x = A.k_pos[(int64_t)key * 3];
         y = A.k_pos[(int64_t)key * 3 + 1];
         z = A.k_pos[(int64_t)key * 3 + 2];
@@ -303,24 +346,69 @@ __global__ __launch_bounds__(64 * ROWW, KMINF) void k_dense_bwd_keys(DenseParams
         };
         tq.load(tid, n, A.D, [&](int r) { return at(A.q, r); });
         tg.load(tid, n, A.D, [&](int r) { return at(A.go, r); });
-        st = make_float4(INFINITY, 0, 0, 0);        // rows behind the end: weight 0
+        st = make_float4(0, 0, 0, INFINITY);        // rows behind the end: weight 0
         if (tid < n && tid < BN) {
             const int in_segment = A.over_group((uint32_t)(t + tid)), head = head_k * A.group + (t + tid - in_segment * A.group);
             const int64_t query = q0 + in_segment;
             st = A.stats[query * Hq + head];
-            if (A.score.biased) {
+            if (BIAS) {
                 rx = A.q_pos[query * 3];
                 ry = A.q_pos[query * 3 + 1];
                 rz = A.q_pos[query * 3 + 2];
-                rs = A.slope[head];
+                rs = A.slope[head] * LOG2E;
             }
         }
     };
     float gx = 0, gy = 0, gz = 0;
-    f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
+    f32x16 dk[NT] = {}, dv[NT] = {};
+    // weights of 32 rows from row m of the tile, left in p (for dv) and ds (for dk)
+    auto weigh = [&](int m, f32x16& p, f32x16& ds) {
+        p = M::dot(qs, m, kf, lane);
+        ds = M::dot(gs, m, vf, lane);
+        f32x16 slack;
+        if (CAP) cap_scores<true>(p, slack, A.score, 0.0f);
+        else plain_scores(p, A.score, 0.0f);
+        float tx = 0, ty = 0, tz = 0;      // a tile's sums by themselves: shorter sums, smaller errors
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            auto line = [&](int l) { return *reinterpret_cast<const f32x4*>(&par[l][m + 4 * half + 8 * b]); };
+            const f32x4 lse = line(ROW_LSE), delta = line(ROW_DELTA);
+            f32x4 px, py, pz, slope;
+            if (BIAS) {
+                px = line(ROW_X);
+                py = line(ROW_Y);
+                pz = line(ROW_Z);
+                slope = line(ROW_SLOPE);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 4 * b + e;
+                float s = p[i] - lse[e], dx, dy, dz, d, id;
+                if (BIAS) {
+                    dx = px[e] - x;
+                    dy = py[e] - y;
+                    dz = pz[e] - z;
+                    distance(dx, dy, dz, d, id);
+                    s -= slope[e] * d;
+                }
+                p[i] = __builtin_amdgcn_exp2f(s);
+                const float g = p[i] * (ds[i] - delta[e]);
+                if (BIAS) {
+                    const float f = g * slope[e] * id;
+                    tx += f * dx;
+                    ty += f * dy;
+                    tz += f * dz;
+                }
+                ds[i] = CAP ? g * slack[i] : g;
+            }
+        }
+        gx += tx;
+        gy += ty;
+        gz += tz;
+    };
     if (begin < end) fetch(begin);
     for (int t = begin; t < end; t += BN) {
-        tile_sync<(ROWW > 1)>();
+        __syncthreads();
         tq.store(tid, qs);
         tg.store(tid, gs);
         if (tid < BN) {
@@ -328,74 +416,75 @@ __global__ __launch_bounds__(64 * ROWW, KMINF) void k_dense_bwd_keys(DenseParams
             par[ROW_Y][tid] = ry;
             par[ROW_Z][tid] = rz;
             par[ROW_SLOPE][tid] = rs;
-            par[ROW_TOP][tid] = st.x;
-            par[ROW_INV][tid] = st.y;
+            par[ROW_LSE][tid] = st.w;
             par[ROW_DELTA][tid] = st.z;
         }
-        tile_sync<(ROWW > 1)>();
+        __syncthreads();
         if (t + BN < end) fetch(t + BN);
-        if (!busy) continue;
-        const int n = min(BN, end - t);
-        for (int m = 0; m < n; m += 32) {
-            f32x16 p = M::dot(qs, m, kf, lane), ds = M::dot(gs, m, vf, lane), slack;
-            cap_scores<true>(p, slack, A.score, 0.0f);
-            float tx = 0, ty = 0, tz = 0;
+        if constexpr (SHARE == 1) {
+            if (!busy) continue;
+            const int n = min(BN, end - t);
+#pragma unroll 1
+            for (int m = 0; m < n; m += 32) {
+                f32x16 p, ds;
+                weigh(m, p, ds);
+                M::accumulate(dv, gs, m, M::weights(p), lane);
+                M::accumulate(dk, qs, m, M::weights(ds), lane);
+            }
+        } else {
+            if (busy) {
+                f32x16 p, ds;
+                weigh(32 * share, p, ds);
+                M::put(&passed[share * KEYW + wave][0][lane], M::weights(p));
+                M::put(&passed[share * KEYW + wave][1][lane], M::weights(ds));
+            }
+            __syncthreads();
+            if (busy) {
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                auto line = [&](int l) { return *reinterpret_cast<const f32x4*>(&par[l][m + 4 * half + 8 * b]); };
-                const f32x4 top = line(ROW_TOP), inv = line(ROW_INV), delta = line(ROW_DELTA);
-                if (A.score.biased) {
-                    const f32x4 px = line(ROW_X), py = line(ROW_Y), pz = line(ROW_Z), slope = line(ROW_SLOPE);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int i = 4 * b + e;
-                        const float dx = px[e] - x, dy = py[e] - y, dz = pz[e] - z;
-                        float d, id;
-                        distance(dx, dy, dz, d, id);
-                        p[i] = __builtin_amdgcn_exp2f((p[i] - top[e]) - slope[e] * LOG2E * d) * inv[e];
-                        const float g = p[i] * (ds[i] - delta[e]), f = g * slope[e] * id;
-                        tx += f * dx;
-                        ty += f * dy;
-                        tz += f * dz;
-                        ds[i] = g;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int i = 4 * b + e;
-                        p[i] = __builtin_amdgcn_exp2f(p[i] - top[e]) * inv[e];
-                        ds[i] = p[i] * (ds[i] - delta[e]);
-                    }
+                for (int u = 0; u < SHARE; ++u) {
+                    M::accumulate(dv, gs + share * NT * 32, 32 * u, M::get(&passed[u * KEYW + wave][0][lane]), lane);
+                    M::accumulate(dk, qs + share * NT * 32, 32 * u, M::get(&passed[u * KEYW + wave][1][lane]), lane);
                 }
             }
-            gx += tx;
-            gy += ty;
-            gz += tz;
-            if (A.score.capped) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) ds[i] *= slack[i];
-            }
-            M::accumulate(dv, gs, m, M::weights(p), lane);
-            M::accumulate(dk, qs, m, M::weights(ds), lane);
         }
     }
     gx += other_half(gx);
     gy += other_half(gy);
     gz += other_half(gz);
+    if constexpr (SHARE > 1 && BIAS) {
+        // the sharing waves' rows together, in their order
+        float* g = reinterpret_cast<float*>(passed);
+        __syncthreads();
+        if (!half) {
+            g[(share * KEYW + wave) * 96 + lane] = gx;
+            g[(share * KEYW + wave) * 96 + 32 + lane] = gy;
+            g[(share * KEYW + wave) * 96 + 64 + lane] = gz;
+        }
+        __syncthreads();
+        if (!half && share == 0) {
+#pragma unroll
+            for (int u = 1; u < SHARE; ++u) {
+                gx += g[(u * KEYW + wave) * 96 + lane];
+                gy += g[(u * KEYW + wave) * 96 + 32 + lane];
+                gz += g[(u * KEYW + wave) * 96 + 64 + lane];
+            }
+        }
+    }
     if (!valid) return;
+    const int d0 = share * NT * 32;
     if (gridDim.y == 1) {
-        store_row<T, DP>(A.gk.row(key, head_k), dk, A.scale, A.D, half);
-        store_row<T, DP>(A.gv.row(key, head_k), dv, 1.0f, A.D, half);
+        store_row<T, NT * 32>(A.gk.row(key, head_k), dk, A.scale, A.D, half, d0);
+        store_row<T, NT * 32>(A.gv.row(key, head_k), dv, 1.0f, A.D, half, d0);
     } else {
         const int64_t at = (((int64_t)blockIdx.y * A.Nk + key) * A.Hk + head_k) * A.D;
-        store_row<float, DP>(reinterpret_cast<char*>(A.gk_part + at), dk, A.scale, A.D, half);
-        store_row<float, DP>(reinterpret_cast<char*>(A.gv_part + at), dv, 1.0f, A.D, half);
+        store_row<float, NT * 32>(reinterpret_cast<char*>(A.gk_part + at), dk, A.scale, A.D, half, d0);
+        store_row<float, NT * 32>(reinterpret_cast<char*>(A.gv_part + at), dv, 1.0f, A.D, half, d0);
     }
-    if (A.k_pos_part && !half) {
+    if (BIAS && A.k_pos_part && !half && share == 0) {
         float* g = A.k_pos_part + (((int64_t)blockIdx.y * A.Hk + head_k) * A.Nk + key) * 3;
-        g[0] = gx;
-        g[1] = gy;
-        g[2] = gz;
+        g[0] = gx * (1.0f / LOG2E);
+        g[1] = gy * (1.0f / LOG2E);
+        g[2] = gz * (1.0f / LOG2E);
     }
 }
 
@@ -456,45 +545,59 @@ __global__ __launch_bounds__(SUM_THREADS) void k_dense_bwd_join(Rows out, const 
     else *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
 }
 
-// Workgroups of four waves and 128 rows (keys), or of one wave where a segment has no more than 64 of them on average; and parts of the
-// other side where these are too few to fill the chip.
+// Workgroups of 128 rows (keys), or of 32 where a segment has no more than 64 of them on average; and parts of the other side
+// where the workgroups do not fill the chip evenly: two of four waves to a compute unit, or one of eight with more than 64 features.
 struct BwdPlan {
-    int row_waves, key_waves, row_parts, key_parts;
+    int row_waves, key_waves, stat_parts, row_parts, key_parts;
     int64_t row_tiles, key_tiles;
 };
-int parts_of(int64_t workgroups, int64_t most) {
-    int64_t parts = workgroups > 0 ? WANT / workgroups : 1;
-    if (parts > most) parts = most;
-    return parts > 64 ? 64 : parts > 1 ? (int)parts : 1;
-}
 BwdPlan bwd_plan(const e2f_dense_args* a) {
     const int group = a->Hq / a->Hk;
     const int64_t S = a->S, rows = (int64_t)a->Nq * group;
-    BwdPlan P = {1, 1, 1, 1, 0, 0};
+    BwdPlan P = {1, 1, 1, 1, 1, 0, 0};
     if (S == 0) return P;
     P.row_waves = rows > 64 * S ? 4 : 1;
     P.key_waves = a->Nk > 64 * S ? 4 : 1;
     P.row_tiles = a->Nq ? dense_tiles(a->Nq, group, a->S, 32 * P.row_waves) : 0;
     P.key_tiles = a->Nk ? dense_tiles(a->Nk, 1, a->S, 32 * P.key_waves) : 0;
-    P.row_parts = parts_of(P.row_tiles * a->Hk * P.row_waves, a->Nk / S / 256);
-    P.key_parts = parts_of(P.key_tiles * a->Hk * P.key_waves, rows / S / 256);
+    // times of a round for a step along the other side, and of a part's sums, written and read at 4.5 TB/s.  At 5 003 keys of 2 heads and
+    // 128 features, 314 workgroups over rows take 475 us in one part, 401 in three and 387 in four; 80 over keys, 20 012 rows, take
+    // 1 600 us in one part and 533 in twelve as in three
+    const double step = a->dtype == E2F_BF16 ? 0.03 + 0.0004 * a->D : 0.05 + 0.004 * a->D;
+    const int slots = a->D > 64 ? 256 : 512;
+    if (P.row_tiles) {
+        const int64_t blocks = P.row_tiles * a->Hk * P.row_waves / 4 + 1, most = a->Nk / S / 256;
+        P.stat_parts = best_parts(blocks, 512, a->Nk / S * step, rows * a->Hk * 32.0 / 4.5e6, most);
+        P.row_parts = best_parts(blocks, slots, a->Nk / S * step, rows * a->Hk * a->D * 8.0 / 4.5e6, most);
+    }
+    if (P.key_tiles) P.key_parts = best_parts(P.key_tiles * a->Hk * P.key_waves / 4 + 1, slots, rows / S * step, (double)a->Nk * a->Hk * a->D * 16.0 / 4.5e6, rows / S / 256);
     return P;
 }
 
 template <typename T, int DP>
 void launch_dp(const DenseParams& A, const BwdPlan& P, hipStream_t st) {
-    const dim3 rows((unsigned)(P.row_tiles * A.Hk), (unsigned)P.row_parts), keys((unsigned)(P.key_tiles * A.Hk), (unsigned)P.key_parts);
+    const dim3 stats((unsigned)(P.row_tiles * A.Hk), (unsigned)P.stat_parts), rows(stats.x, (unsigned)P.row_parts),
+        keys((unsigned)(P.key_tiles * A.Hk), (unsigned)P.key_parts);
     const int64_t n = (int64_t)A.Nq * A.Hk * A.group;
+    // more than 64 features: two waves to a group of rows or keys
+    constexpr int KD = DP > 64 ? 128 : DP, SHARE = DP > 64 ? 2 : 1;
     if (rows.x) {
-        if (P.row_waves == 4) k_dense_bwd_stats<T, DP, 4><<<rows, 256, 0, st>>>(A);
-        else k_dense_bwd_stats<T, DP, 1><<<rows, 64, 0, st>>>(A);
-        if (P.row_parts > 1) k_dense_bwd_join_stats<<<(unsigned)((n + SUM_THREADS - 1) / SUM_THREADS), SUM_THREADS, 0, st>>>(A, P.row_parts);
-        if (P.row_waves == 4) k_dense_bwd_rows<T, DP, 4><<<rows, 256, 0, st>>>(A);
-        else k_dense_bwd_rows<T, DP, 1><<<rows, 64, 0, st>>>(A);
+        if (P.row_waves == 4) k_dense_bwd_stats<T, DP, 4><<<stats, 256, 0, st>>>(A);
+        else k_dense_bwd_stats<T, DP, 1><<<stats, 64, 0, st>>>(A);
+        if (P.stat_parts > 1) k_dense_bwd_join_stats<<<(unsigned)((n + SUM_THREADS - 1) / SUM_THREADS), SUM_THREADS, 0, st>>>(A, P.stat_parts);
+        if (P.row_waves == 4) k_dense_bwd_rows<T, KD, 4, SHARE><<<rows, 256 * SHARE, 0, st>>>(A);
+        else k_dense_bwd_rows<T, KD, 1, SHARE><<<rows, 64 * SHARE, 0, st>>>(A);
     }
     if (keys.x) {
-        if (P.key_waves == 4) k_dense_bwd_keys<T, DP, 4><<<keys, 256, 0, st>>>(A);
-        else k_dense_bwd_keys<T, DP, 1><<<keys, 64, 0, st>>>(A);
+        auto go = [&](auto cap, auto bias) {
+            constexpr bool CAP = decltype(cap)::value, BIAS = decltype(bias)::value;
+            if (P.key_waves == 4) k_dense_bwd_keys<T, KD, 4, SHARE, CAP, BIAS><<<keys, 256 * SHARE, 0, st>>>(A);
+            else k_dense_bwd_keys<T, KD, 1, SHARE, CAP, BIAS><<<keys, 64 * SHARE, 0, st>>>(A);
+        };
+        const std::true_type yes;
+        const std::false_type no;
+        if (A.score.capped) A.score.biased ? go(yes, yes) : go(yes, no);
+        else A.score.biased ? go(no, yes) : go(no, no);
     }
     auto join = [&](const Rows& out, const float* part, int parts, const int32_t* offsets, const int32_t* lengths, int N, int H) {
         const int64_t threads = (int64_t)N * H * (A.D / 4);
@@ -524,12 +627,12 @@ size_t layout(const e2f_dense_args* a, const BwdPlan& P, char* ws, DenseParams* 
         off += e2f_align_up(floats * sizeof(float));
         return reinterpret_cast<float*>(p);
     };
-    const size_t rows = (size_t)a->Nq * a->Hq, keys = (size_t)a->Nk * a->Hk, rp = P.row_parts, kp = P.key_parts;
+    const size_t rows = (size_t)a->Nq * a->Hq, keys = (size_t)a->Nk * a->Hk, sp = P.stat_parts, rp = P.row_parts, kp = P.key_parts;
     float* stats = take(rows * 4);
     float* slope = take(a->slope ? rp * P.row_tiles * a->Hq : 0);
     float* qp = take(a->slope ? rp * rows * 3 : 0);
     float* kpos = take(a->slope ? kp * keys * 3 : 0);
-    float* stats_part = take(rp > 1 ? rp * rows * 4 : 0);
+    float* stats_part = take(sp > 1 ? sp * rows * 4 : 0);
     float* gq = take(rp > 1 ? rp * rows * a->D : 0);
     float* gk = take(kp > 1 ? kp * keys * a->D : 0);
     float* gv = take(kp > 1 ? kp * keys * a->D : 0);
