@@ -372,40 +372,39 @@ def e2f_eaas_tensor_product(ctx, h, r, w_path, out):
 ROTARY = {"half": 0, "interleaved": 1}
 
 
-def _need(ok, where):
-    if not ok:
-        raise E2fError(E2F_ERR_INVALID_ARG, where)
+def _refuse(where):
+    raise E2fError(E2F_ERR_INVALID_ARG, where)
 
 
 def _feature_type(t, where):
     import torch
-    _need(t.dtype in (torch.float32, torch.bfloat16), where)
+    if t.dim() != 3 or t.dtype not in (torch.float32, torch.bfloat16):
+        _refuse(where)
     return E2F_BF16 if t.dtype == torch.bfloat16 else E2F_F32
 
 
-def _heads(t, like, shape, where):
-    """[N][H][D] tensor of the type and on the device of `like`, features side by side -> Heads."""
-    if t.shape != shape or t.dtype != like.dtype or t.device != like.device:
-        _need(False, where)
+def _heads(t, dtype, device, shape, where, name):
+    """[N][H][D] tensor of a type on a device, features side by side -> Heads."""
+    if t.shape != shape or t.dtype != dtype or t.device != device:
+        _refuse(f"{where}: {name}")
     token, head, feature = t.stride()
     if feature != 1 and shape[2] > 1:
-        _need(False, where)
+        _refuse(f"{where}: {name}")
     return Heads(t.data_ptr(), token, head)
 
 
-def _plain(t, like, dtype, shape, where):
-    """Contiguous tensor of a type and shape on the device of `like` -> its address; None -> None."""
-    if t is None:
-        return None
-    if t.dtype != dtype or t.shape != shape or t.device != like.device or not t.is_contiguous():
-        _need(False, where)
+def _plain(t, dtype, device, shape, where, name):
+    """Contiguous tensor of a type and shape on a device -> its address."""
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        _refuse(f"{where}: {name}")
     return t.data_ptr()
 
 
 def _on(device, call, *args):
     """call(*args, stream) with the device current."""
     import torch
-    _need(device.type == "cuda", call.__name__)
+    if device.type != "cuda":
+        _refuse(call.__name__)
     at = device.index
     if at == torch.cuda.current_device():
         return call(*args, _raw_stream(at))
@@ -414,52 +413,58 @@ def _on(device, call, *args):
 
 
 def _raw_stream(index):
-    """The current stream's handle; without making a Stream object (2 us of a call's 15) where this torch can."""
+    """The current stream's handle; without making a Stream object (2 us of a call's 10) where this torch can."""
     import torch
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
 
 
-def _bytes_of(ws, like, where):
+def _bytes_of(ws, device, where):
     import torch
-    _need(ws is None or (ws.dtype == torch.uint8 and ws.device == like.device and ws.is_contiguous()), where)
-    return (ws.data_ptr(), ws.numel()) if ws is not None else (None, 0)
+    if ws is None:
+        return None, 0
+    if ws.dtype != torch.uint8 or ws.device != device or not ws.is_contiguous():
+        _refuse(f"{where}: ws")
+    return ws.data_ptr(), ws.numel()
 
 
-def _qk_args(where, q, k, position, weight_q, weight_k, rotary_dim, layout, theta, position_scale, eps):
+def _qk_args(where, q, k, position=None, weight_q=None, weight_k=None, rotary_dim=0, layout=0, theta=1.0, position_scale=1.0,
+             eps=1.0):
+    """(QkArgs, type, device, shape of q, shape of k)"""
     import torch
-    _need(q is not None or k is not None, where)
     x = q if q is not None else k
-    _need(x.dim() == 3, where)
-    N, D = x.shape[0], x.shape[2]
-    a = QkArgs(_feature_type(x, where), N, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], D, rotary_dim,
-               ROTARY.get(layout, layout), eps, theta, position_scale,
-               _plain(position, x, torch.int32, (N,), where + ": position"),
-               _plain(weight_q, x, torch.float32, (D,), where + ": weight_q"),
-               _plain(weight_k, x, torch.float32, (D,), where + ": weight_k"))
-    return a, x, (N, a.Hq, D), (N, a.Hk, D)
+    if x is None:
+        _refuse(where)
+    kind, device, f32 = _feature_type(x, where), x.device, torch.float32
+    N, _, D = x.shape
+    Hq, Hk = 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
+    a = QkArgs(kind, N, Hq, Hk, D, rotary_dim, ROTARY.get(layout, layout), eps, theta, position_scale,
+               None if position is None else _plain(position, torch.int32, device, (N,), where, "position"),
+               None if weight_q is None else _plain(weight_q, f32, device, (D,), where, "weight_q"),
+               None if weight_k is None else _plain(weight_k, f32, device, (D,), where, "weight_k"))
+    return a, x.dtype, device, (N, Hq, D), (N, Hk, D)
 
 
-def _optional_heads(t, like, shape, where):
+def _optional_heads(t, dtype, device, shape, where, name):
     if shape[1] == 0:
         return Heads()
-    _need(t is not None, where)
-    return _heads(t, like, shape, where)
+    if t is None:
+        _refuse(f"{where}: {name}")
+    return _heads(t, dtype, device, shape, where, name)
 
 
 def e2f_qk_norm_rotate(q, k, q_out, k_out, position=None, weight_q=None, weight_k=None, rotary_dim=0, layout="half",
                        theta=10000.0, position_scale=1.0, eps=1e-6):
     """q [N][Hq][D], k [N][Hk][D] (either may be None), q_out, k_out alike; position int32 [N]; weights float32 [D]."""
     where = "e2f_qk_norm_rotate"
-    a, x, sq, sk = _qk_args(where, q, k, position, weight_q, weight_k, rotary_dim, layout, theta, position_scale, eps)
-    rows = [_optional_heads(t, x, s, where + ": " + n)
-            for t, s, n in ((q, sq, "q"), (k, sk, "k"), (q_out, sq, "q_out"), (k_out, sk, "k_out"))]
-    _check(_on(x.device, load().e2f_qk_norm_rotate, a, *rows), where)
+    a, dt, dev, sq, sk = _qk_args(where, q, k, position, weight_q, weight_k, rotary_dim, layout, theta, position_scale, eps)
+    _check(_on(dev, load().e2f_qk_norm_rotate, a, _optional_heads(q, dt, dev, sq, where, "q"),
+               _optional_heads(k, dt, dev, sk, where, "k"), _optional_heads(q_out, dt, dev, sq, where, "q_out"),
+               _optional_heads(k_out, dt, dev, sk, where, "k_out")), where)
 
 
 def e2f_qk_norm_rotate_backward_workspace_bytes(q, k):
-    a = _qk_args("e2f_qk_norm_rotate_backward_workspace_bytes", q, k, None, None, None, 0, 0, 1.0, 1.0, 1.0)[0]
-    return load().e2f_qk_norm_rotate_backward_workspace_bytes(a)
+    return load().e2f_qk_norm_rotate_backward_workspace_bytes(_qk_args("e2f_qk_norm_rotate_backward_workspace_bytes", q, k)[0])
 
 
 def e2f_qk_norm_rotate_backward(q, k, grad_q_out, grad_k_out, grad_q, grad_k, grad_weight_q, grad_weight_k, ws, position=None,
@@ -468,30 +473,47 @@ def e2f_qk_norm_rotate_backward(q, k, grad_q_out, grad_k_out, grad_q, grad_k, gr
     """grad_weight_q, grad_weight_k float32 [D] or None; ws uint8."""
     import torch
     where = "e2f_qk_norm_rotate_backward"
-    a, x, sq, sk = _qk_args(where, q, k, position, weight_q, weight_k, rotary_dim, layout, theta, position_scale, eps)
-    rows = [_optional_heads(t, x, s, where + ": " + n)
+    a, dt, dev, sq, sk = _qk_args(where, q, k, position, weight_q, weight_k, rotary_dim, layout, theta, position_scale, eps)
+    rows = [_optional_heads(t, dt, dev, s, where, n)
             for t, s, n in ((q, sq, "q"), (k, sk, "k"), (grad_q_out, sq, "grad_q_out"), (grad_k_out, sk, "grad_k_out"),
                             (grad_q, sq, "grad_q"), (grad_k, sk, "grad_k"))]
-    sums = [_plain(t, x, torch.float32, (a.D,), where + ": grad_weight") for t in (grad_weight_q, grad_weight_k)]
-    _check(_on(x.device, load().e2f_qk_norm_rotate_backward, a, *rows, *sums, *_bytes_of(ws, x, where + ": ws")), where)
+    sums = [None if t is None else _plain(t, torch.float32, dev, (a.D,), where, "grad_weight") for t in (grad_weight_q, grad_weight_k)]
+    _check(_on(dev, load().e2f_qk_norm_rotate_backward, a, *rows, *sums, *_bytes_of(ws, dev, where)), where)
 
 
-def _dense_args(where, q, k, S, q_offsets=None, k_offsets=None, scale=None, cap=0.0, q_pos=None, k_pos=None, slope=None,
-                q_lengths=None, k_lengths=None):
-    import torch
-    _need(q.dim() == 3 and k.dim() == 3, where)
+def _dense_sizes(where, q, k, S):
+    kind = _feature_type(q, where)
+    if k.dim() != 3:
+        _refuse(f"{where}: k")
     (Nq, Hq, D), (Nk, Hk, _) = q.shape, k.shape
-    ints = [_plain(t, q, torch.int32, (n,), where + ": " + name)
-            for t, n, name in ((q_offsets, S + 1, "q_offsets"), (k_offsets, S + 1, "k_offsets"),
-                               (q_lengths, S, "q_lengths"), (k_lengths, S, "k_lengths"))]
-    floats = [_plain(t, q, torch.float32, shape, where + ": " + name)
-              for t, shape, name in ((q_pos, (Nq, 3), "q_pos"), (k_pos, (Nk, 3), "k_pos"), (slope, (Hq,), "slope"))]
-    return DenseArgs(_feature_type(q, where), Hq, Hk, D, Nq, Nk, S, D ** -0.5 if scale is None else scale, cap, *ints, *floats)
+    return DenseArgs(kind, Hq, Hk, D, Nq, Nk, S, 1.0, 0.0)
+
+
+def _dense_args(where, q, k, q_offsets, k_offsets, scale, cap, q_pos, k_pos, slope, q_lengths, k_lengths):
+    import torch
+    if q_offsets.dim() != 1 or q_offsets.shape[0] == 0:
+        _refuse(f"{where}: q_offsets")
+    S, dev, i32, f32 = q_offsets.shape[0] - 1, q.device, torch.int32, torch.float32
+    a = _dense_sizes(where, q, k, S)
+    a.scale, a.cap = a.D ** -0.5 if scale is None else scale, cap
+    a.q_offsets = _plain(q_offsets, i32, dev, (S + 1,), where, "q_offsets")
+    a.k_offsets = _plain(k_offsets, i32, dev, (S + 1,), where, "k_offsets")
+    if q_lengths is not None:
+        a.q_lengths = _plain(q_lengths, i32, dev, (S,), where, "q_lengths")
+    if k_lengths is not None:
+        a.k_lengths = _plain(k_lengths, i32, dev, (S,), where, "k_lengths")
+    if slope is not None:
+        a.slope = _plain(slope, f32, dev, (a.Hq,), where, "slope")
+    if q_pos is not None:
+        a.q_pos = _plain(q_pos, f32, dev, (a.Nq, 3), where, "q_pos")
+    if k_pos is not None:
+        a.k_pos = _plain(k_pos, f32, dev, (a.Nk, 3), where, "k_pos")
+    return a
 
 
 def e2f_dense_attn_workspace_bytes(q, k, S):
     """S segments."""
-    return load().e2f_dense_attn_workspace_bytes(_dense_args("e2f_dense_attn_workspace_bytes", q, k, S))
+    return load().e2f_dense_attn_workspace_bytes(_dense_sizes("e2f_dense_attn_workspace_bytes", q, k, S))
 
 
 def e2f_dense_attn_forward(q, k, v, q_offsets, k_offsets, out, ws, scale=None, cap=0.0, q_pos=None, k_pos=None, slope=None,
@@ -499,15 +521,15 @@ def e2f_dense_attn_forward(q, k, v, q_offsets, k_offsets, out, ws, scale=None, c
     """q, out [Nq][Hq][D]; k, v [Nk][Hk][D]; q_offsets, k_offsets int32 [S+1]; q_lengths, k_lengths int32 [S] or None;
     q_pos, k_pos float32 [Nq][3], [Nk][3] and slope float32 [Hq], or None; scale: 1/sqrt(D) unless given; ws uint8."""
     where = "e2f_dense_attn_forward"
-    a = _dense_args(where, q, k, q_offsets.shape[0] - 1, q_offsets, k_offsets, scale, cap, q_pos, k_pos, slope, q_lengths, k_lengths)
-    sq, sk = (a.Nq, a.Hq, a.D), (a.Nk, a.Hk, a.D)
-    rows = [_heads(t, q, s, where + ": " + n) for t, s, n in ((q, sq, "q"), (k, sk, "k"), (v, sk, "v"), (out, sq, "out"))]
-    _check(_on(q.device, load().e2f_dense_attn_forward, a, *rows, *_bytes_of(ws, q, where + ": ws")), where)
+    a = _dense_args(where, q, k, q_offsets, k_offsets, scale, cap, q_pos, k_pos, slope, q_lengths, k_lengths)
+    dt, dev, sq, sk = q.dtype, q.device, (a.Nq, a.Hq, a.D), (a.Nk, a.Hk, a.D)
+    _check(_on(dev, load().e2f_dense_attn_forward, a, _heads(q, dt, dev, sq, where, "q"), _heads(k, dt, dev, sk, where, "k"),
+               _heads(v, dt, dev, sk, where, "v"), _heads(out, dt, dev, sq, where, "out"), *_bytes_of(ws, dev, where)), where)
 
 
 def e2f_dense_attn_backward_workspace_bytes(q, k, S):
     """S segments; the size that serves a call with or without slope."""
-    a = _dense_args("e2f_dense_attn_backward_workspace_bytes", q, k, S)
+    a = _dense_sizes("e2f_dense_attn_backward_workspace_bytes", q, k, S)
     a.slope = 4096      # not followed: whether there is one counts
     return load().e2f_dense_attn_backward_workspace_bytes(a)
 
@@ -518,15 +540,15 @@ def e2f_dense_attn_backward(q, k, v, q_offsets, k_offsets, grad_out, grad_q, gra
     """As e2f_dense_attn_forward; grad_slope float32 [Hq], grad_q_pos [Nq][3], grad_k_pos [Nk][3] or None."""
     import torch
     where = "e2f_dense_attn_backward"
-    a = _dense_args(where, q, k, q_offsets.shape[0] - 1, q_offsets, k_offsets, scale, cap, q_pos, k_pos, slope, q_lengths, k_lengths)
-    sq, sk = (a.Nq, a.Hq, a.D), (a.Nk, a.Hk, a.D)
-    rows = [_heads(t, q, s, where + ": " + n)
+    a = _dense_args(where, q, k, q_offsets, k_offsets, scale, cap, q_pos, k_pos, slope, q_lengths, k_lengths)
+    dt, dev, sq, sk = q.dtype, q.device, (a.Nq, a.Hq, a.D), (a.Nk, a.Hk, a.D)
+    rows = [_heads(t, dt, dev, s, where, n)
             for t, s, n in ((q, sq, "q"), (k, sk, "k"), (v, sk, "v"), (grad_out, sq, "grad_out"), (grad_q, sq, "grad_q"),
                             (grad_k, sk, "grad_k"), (grad_v, sk, "grad_v"))]
-    sums = [_plain(t, q, torch.float32, s, where + ": " + n)
+    sums = [None if t is None else _plain(t, torch.float32, dev, s, where, n)
             for t, s, n in ((grad_slope, (a.Hq,), "grad_slope"), (grad_q_pos, (a.Nq, 3), "grad_q_pos"),
                             (grad_k_pos, (a.Nk, 3), "grad_k_pos"))]
-    _check(_on(q.device, load().e2f_dense_attn_backward, a, *rows, *sums, *_bytes_of(ws, q, where + ": ws")), where)
+    _check(_on(dev, load().e2f_dense_attn_backward, a, *rows, *sums, *_bytes_of(ws, dev, where)), where)
 
 
 def e2f_grad_norm_clip_workspace_bytes(grads):
@@ -538,18 +560,19 @@ def e2f_grad_norm_clip(grads, out, max_norm, norm, ws):
     """grads, out: lists of contiguous float32 or bfloat16 tensors (out may be grads); norm float32 [1]; ws uint8."""
     import torch
     where = "e2f_grad_norm_clip"
-    n = len(grads)
-    _need(len(out) == n, where + ": out")
-    _need(norm.dtype == torch.float32 and norm.numel() == 1, where + ": norm")
+    n, dev = len(grads), norm.device
+    if len(out) != n or norm.dtype != torch.float32 or norm.numel() != 1:
+        _refuse(where)
     types = {torch.float32: E2F_F32, torch.bfloat16: E2F_BF16}
-    for g, o in zip(grads, out):
-        _need(g.dtype in types and o.dtype == g.dtype and o.shape == g.shape and g.device == o.device == norm.device and
-              g.is_contiguous() and o.is_contiguous(), where)
+    kinds = [types.get(g.dtype, -1) for g in grads]
+    counts = [g.numel() for g in grads]
+    for g, o, kind in zip(grads, out, kinds):
+        if kind < 0 or o.dtype != g.dtype or o.shape != g.shape or g.device != dev or o.device != dev or not (
+                g.is_contiguous() and o.is_contiguous()):
+            _refuse(where)
     pointers = ctypes.c_void_p * n
-    _check(_on(norm.device, load().e2f_grad_norm_clip, n, pointers(*[g.data_ptr() for g in grads]),
-               pointers(*[o.data_ptr() for o in out]), (ctypes.c_int64 * n)(*[g.numel() for g in grads]),
-               (ctypes.c_int32 * n)(*[types[g.dtype] for g in grads]), max_norm, norm.data_ptr(),
-               *_bytes_of(ws, norm, where + ": ws")), where)
+    _check(_on(dev, load().e2f_grad_norm_clip, n, pointers(*[g.data_ptr() for g in grads]), pointers(*[o.data_ptr() for o in out]),
+               (ctypes.c_int64 * n)(*counts), (ctypes.c_int32 * n)(*kinds), max_norm, norm.data_ptr(), *_bytes_of(ws, dev, where)), where)
 
 
 def e2f_profile_begin(ctx, max_calls):
