@@ -53,23 +53,44 @@ __device__ __forceinline__ void segment_range(const int32_t* offsets, const int3
 // Tiles are numbered so that no table is needed: with rows = tokens * group, segment s starts at tile
 // floor(rows before it / BM) + s, which leaves it at least as many tiles as it has rows for, since
 // floor(a + b) - floor(a) + 1 >= ceil(b).  The whole wave looks for the segment, 64 candidates at a time.
-__device__ __forceinline__ int64_t first_tile(const int32_t* offsets, int s, int N, int group, int BM) {
-    return (int64_t)min(max(offsets[s], 0), N) * group / BM + s;
+__device__ __forceinline__ int64_t first_tile(int offset, int s, int N, int group, int BM) {
+    return ((int64_t)min(max(offset, 0), N) * group >> (BM == 128 ? 7 : 5)) + s;
 }
 static inline int64_t dense_tiles(int64_t N, int group, int S, int BM) { return N * group / BM + S; }
 
-__device__ __forceinline__ int segment_of(const int32_t* offsets, int S, int N, int group, int BM, int64_t tile) {
-    int lo = 0, n = S;             // the answer lies in [lo, lo + n)
-    const int lane = threadIdx.x & 63;
-    while (n > 1) {
+struct Segment {
+    int q0, nq, k0, nk;            // first query, queries, first key, keys
+    int64_t first;                 // first tile
+};
+// KEYS: tiles of keys instead of rows.  The last round reads all that is wanted of its 63 candidates, so that a workgroup among up to 63
+// segments waits for memory once.
+template <bool KEYS>
+__device__ __forceinline__ Segment segment_of(const DenseParams& A, int BM, int64_t tile) {
+    const int32_t* offsets = KEYS ? A.k_offsets : A.q_offsets;
+    const int N = KEYS ? A.Nk : A.Nq, group = KEYS ? 1 : A.group, lane = threadIdx.x & 63;
+    int lo = 0, n = A.S;           // the answer lies in [lo, lo + n)
+    while (n > 63) {
         const int step = (n + 63) / 64, at = lo + lane * step;
-        const bool before = lane * step < n && first_tile(offsets, at, N, group, BM) <= tile;
-        const int k = __popcll(__ballot(before));          // candidate 0 always counts
-        const int next = lo + (k ? k - 1 : 0) * step;
+        const bool before = lane * step < n && first_tile(offsets[min(at, A.S)], at, N, group, BM) <= tile;
+        const int k = __popcll(__ballot(before)), next = lo + (k ? k - 1 : 0) * step;      // candidate 0 always counts
         n = min(step, lo + n - next);
         lo = next;
     }
-    return __builtin_amdgcn_readfirstlane(lo);
+    const int at = lo + min(lane, n);
+    const int q = A.q_offsets[at], k = A.k_offsets[at];
+    int lq = INT32_MAX, lk = INT32_MAX;
+    if (A.q_lengths) lq = A.q_lengths[min(at, A.S - 1)];
+    if (A.k_lengths) lk = A.k_lengths[min(at, A.S - 1)];
+    const int64_t first = first_tile(KEYS ? k : q, at, N, group, BM);
+    const int found = max(__popcll(__ballot(lane < n && first <= tile)) - 1, 0);
+    auto of = [&](int x, int i) { return __builtin_amdgcn_readlane(x, i); };
+    Segment s;
+    s.q0 = min(max(of(q, found), 0), A.Nq);
+    s.nq = min(max(of(lq, found), 0), min(max(of(q, found + 1), s.q0), A.Nq) - s.q0);
+    s.k0 = min(max(of(k, found), 0), A.Nk);
+    s.nk = min(max(of(lk, found), 0), min(max(of(k, found + 1), s.k0), A.Nk) - s.k0);
+    s.first = first_tile(KEYS ? s.k0 : s.q0, __builtin_amdgcn_readfirstlane(lo) + found, N, group, BM);
+    return s;
 }
 
 // The last segment that starts at or before a token.

@@ -47,11 +47,10 @@ struct RowWalk {
         share = (threadIdx.x >> 6) / ROWW;
         head_k = blockIdx.x % A.Hk;
         const int64_t tile = blockIdx.x / A.Hk;
-        const int s = segment_of(A.q_offsets, A.S, A.Nq, A.group, BM, tile);
-        int q0, nq, nk;
-        segment_range(A.q_offsets, A.q_lengths, s, A.Nq, q0, nq);
-        segment_range(A.k_offsets, A.k_lengths, s, A.Nk, k0, nk);
-        const int64_t row0 = (tile - first_tile(A.q_offsets, s, A.Nq, A.group, BM)) * BM, rows = (int64_t)nq * A.group;
+        const Segment segment = segment_of<false>(A, BM, tile);
+        const int q0 = segment.q0, nq = segment.nq, nk = segment.nk;
+        k0 = segment.k0;
+        const int64_t row0 = (tile - segment.first) * BM, rows = (int64_t)nq * A.group;
         any = row0 >= 0 && row0 < rows;
         if (!any) return;
         first_head = (int)(row0 % A.group);
@@ -115,7 +114,7 @@ struct RowWalk {
 
 // Softmax statistics of the rows: reference, sum, sum of p dp.  With parts of the keys each leaves its own, [parts][Nq][Hq].
 template <typename T, int DP, int ROWW>
-__global__ __launch_bounds__(64 * ROWW, 2) void k_dense_bwd_stats(DenseParams A) {
+__global__ __launch_bounds__(64 * ROWW, ROWW == 1 && DP * sizeof(T) > 256 ? 1 : 2) void k_dense_bwd_stats(DenseParams A) {
     using R = RowWalk<T, DP, ROWW, 1>;
     using M = typename R::M;
     __shared__ __align__(16) typename R::Tile tile;
@@ -173,7 +172,7 @@ __global__ __launch_bounds__(SUM_THREADS) void k_dense_bwd_join_stats(DenseParam
 // dq and a row's shares of the gradients of slope and place, from the statistics.  SHARE waves to a group of rows pass each other the
 // weights and keep the sums of DP / SHARE features each, as in the kernel over keys.
 template <typename T, int DP, int ROWW, int SHARE>
-__global__ __launch_bounds__(64 * ROWW * SHARE, DP * sizeof(T) / SHARE <= 256 ? 2 : 1) void k_dense_bwd_rows(DenseParams A) {
+__global__ __launch_bounds__(64 * ROWW * SHARE, ROWW == 1 && DP * sizeof(T) > 128 ? 1 : 2) void k_dense_bwd_rows(DenseParams A) {
     using R = RowWalk<T, DP, ROWW, SHARE>;
     using M = typename R::M;
     constexpr int BN = R::BN, NT = DP / SHARE / 32;
@@ -302,7 +301,7 @@ enum { ROW_X, ROW_Y, ROW_Z, ROW_SLOPE, ROW_LSE, ROW_DELTA, ROW_LINES };
 // tile, pass each other the weights through LDS and keep the sums of DP / SHARE features each.  With 128 features one wave's operands and sums
 // take more registers than leave room for a second wave on its SIMD.
 template <typename T, int DP, int KEYW, int SHARE, bool CAP, bool BIAS>
-__global__ __launch_bounds__(64 * KEYW * SHARE, 2) void k_dense_bwd_keys(DenseParams A) {
+__global__ __launch_bounds__(64 * KEYW * SHARE, KEYW == 1 && DP * sizeof(T) > 128 ? 1 : 2) void k_dense_bwd_keys(DenseParams A) {
     using M = Mma<T, DP>;
     constexpr int BN = SHARE > 1 ? 32 * SHARE : KEYW > 1 && sizeof(T) == 2 ? 64 : 32, BM = 32 * KEYW, THREADS = 64 * KEYW * SHARE;
     constexpr int NT = DP / SHARE / 32;
@@ -313,11 +312,9 @@ __global__ __launch_bounds__(64 * KEYW * SHARE, 2) void k_dense_bwd_keys(DensePa
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = (tid >> 6) % KEYW, share = (tid >> 6) / KEYW;
     const int head_k = blockIdx.x % A.Hk, Hq = A.Hk * A.group;
     const int64_t tile = blockIdx.x / A.Hk;
-    const int s = segment_of(A.k_offsets, A.S, A.Nk, 1, BM, tile);
-    int q0, nq, k0, nk;
-    segment_range(A.q_offsets, A.q_lengths, s, A.Nq, q0, nq);
-    segment_range(A.k_offsets, A.k_lengths, s, A.Nk, k0, nk);
-    const int64_t first = (tile - first_tile(A.k_offsets, s, A.Nk, 1, BM)) * BM;
+    const Segment segment = segment_of<true>(A, BM, tile);
+    const int q0 = segment.q0, nq = segment.nq, k0 = segment.k0, nk = segment.nk;
+    const int64_t first = (tile - segment.first) * BM;
     const int rows = nq * A.group;
     if (first < 0 || first >= nk) return;
     const int mine = (int)first + wave * 32 + (lane & 31);

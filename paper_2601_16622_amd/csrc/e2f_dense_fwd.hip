@@ -19,7 +19,7 @@ struct FwdShape {
 };
 
 template <typename T, int DP, int ROWW, int KEYW>
-__global__ __launch_bounds__(64 * ROWW * KEYW, 2) void k_dense_fwd(DenseParams A) {
+__global__ __launch_bounds__(64 * ROWW * KEYW, ROWW == 1 && DP * sizeof(T) > 128 ? 1 : 2) void k_dense_fwd(DenseParams A) {
     using F = FwdShape<T, DP, ROWW, KEYW>;
     using M = typename F::M;
     constexpr int BN = F::BN;
@@ -30,11 +30,9 @@ __global__ __launch_bounds__(64 * ROWW * KEYW, 2) void k_dense_fwd(DenseParams A
     typename F::Tile& tile = tiles[keyw];
     const int head_k = blockIdx.x % A.Hk;
     const int64_t t_index = blockIdx.x / A.Hk;
-    const int s = segment_of(A.q_offsets, A.S, A.Nq, A.group, F::BM, t_index);
-    int q0, nq, k0, nk;
-    segment_range(A.q_offsets, A.q_lengths, s, A.Nq, q0, nq);
-    segment_range(A.k_offsets, A.k_lengths, s, A.Nk, k0, nk);
-    const int64_t row0 = (t_index - first_tile(A.q_offsets, s, A.Nq, A.group, F::BM)) * F::BM, rows = (int64_t)nq * A.group;
+    const Segment segment = segment_of<false>(A, F::BM, t_index);
+    const int q0 = segment.q0, nq = segment.nq, k0 = segment.k0, nk = segment.nk;
+    const int64_t row0 = (t_index - segment.first) * F::BM, rows = (int64_t)nq * A.group;
     if (row0 < 0 || row0 >= rows) return;
     const int64_t row = row0 + roww * 32 + (lane & 31);
     const bool valid = row < rows, busy = row0 + roww * 32 < rows;
@@ -211,14 +209,21 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_dense_join(DenseParams A, i
             if (f >= 0.0f || f != f) sum += f * of[1];
         }
         const int m = min(64, p1 - q);
-#pragma unroll 16
-        for (int i = 0; i < m; ++i) {
-            const float g = __shfl(f, i);
-            const float* part = A.part + ((q + i) * stride + row) * A.D;
-            const bool in = !(g < 0.0f);
-            const float x0 = in && lane < A.D ? part[lane] : 0.0f, x1 = in && lane + 64 < A.D ? part[lane + 64] : 0.0f;
-            a0 += in ? g * x0 : 0.0f;
-            a1 += in ? g * x1 : 0.0f;
+        for (int i = 0; i < m; i += 16) {
+            float x[16], y[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float* part = A.part + ((q + i + j) * stride + row) * A.D;
+                const bool in = i + j < m && !(__shfl(f, i + j) < 0.0f);
+                x[j] = in && lane < A.D ? part[lane] : 0.0f;
+                y[j] = in && lane + 64 < A.D ? part[lane + 64] : 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float g = i + j < m ? __shfl(f, i + j) : -1.0f;
+                a0 += g < 0.0f ? 0.0f : g * x[j];
+                a1 += g < 0.0f ? 0.0f : g * y[j];
+            }
         }
     }
 #pragma unroll
