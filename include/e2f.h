@@ -347,8 +347,9 @@ e2f_status e2f_eaas_tensor_product(e2f_ctx *ctx, const void *h, const float *r, 
  * paper's operator, which it leaves as it is).  Its operands are rows of heads, element (token t, head h, feature d) at
  * ptr[t * token_stride + h * head_stride + d]; the strides count elements.
  *   ptr           device, 16-byte aligned
- *   token_stride, head_stride  >= 0 and multiples of 16 bytes: E2F_ERR_UNSUPPORTED otherwise.  A stride of 0 repeats a
- *                 row and is for operands that are read; rows of a result must not overlap (E2F_ERR_INVALID_ARG).
+ *   token_stride, head_stride  >= 0; multiples of 16 bytes, the first below 2^25 bytes: E2F_ERR_UNSUPPORTED otherwise.  A
+ *                 stride of 0 repeats a row and is for operands that are read; rows of a result must not overlap
+ *                 (E2F_ERR_INVALID_ARG).
  * None of these calls allocates or synchronises, so all of them can be captured into a graph; a graph keeps the
  * workspace that it was captured with, and two calls that overlap in time need a workspace each.  The device that
  * hip_stream belongs to must be the current device.  Results do not depend on the order in which workgroups run.

@@ -19,6 +19,8 @@ static inline e2f_status check_rows(const e2f_heads* x, int32_t dtype, int64_t N
     // the last element's byte offset has to be a 63-bit number
     const int64_t far = INT64_MAX / 8;
     if ((N > 1 && x->token_stride > far / N) || (H > 1 && x->head_stride > far / H)) return E2F_ERR_INVALID_ARG;
+    // kernels form offsets of up to 64 rows in 32 bits
+    if (N > 1 && x->token_stride * elem_bytes(dtype) >= (1 << 25)) return E2F_ERR_UNSUPPORTED;
     return E2F_OK;
 }
 

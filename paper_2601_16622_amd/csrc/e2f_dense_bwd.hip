@@ -80,10 +80,12 @@ struct RowWalk {
         const int tid = threadIdx.x;
         Transfer<M, DP, BN, THREADS> tk, tv;
         PlaceTransfer<BN, THREADS> tp;
+        tk.place(tid, A.k.token_bytes);
+        tv.place(tid, A.v.token_bytes);
         auto fetch = [&](int t) {
             const int n = end - t;
-            tk.load(tid, n, A.D, [&](int r) { return A.k.row(k0 + t + r, head_k); });
-            tv.load(tid, n, A.D, [&](int r) { return A.v.row(k0 + t + r, head_k); });
+            tk.load(A.k.row(k0 + t, head_k), tid, n, A.D);
+            tv.load(A.v.row(k0 + t, head_k), tid, n, A.D);
             if (A.score.biased) tp.load(tid, min(n, BN), A.k_pos + (int64_t)(k0 + t) * 3);
         };
         if (begin < end) fetch(begin);
@@ -341,8 +343,8 @@ __global__ __launch_bounds__(64 * KEYW * SHARE, KEYW == 1 && DP * sizeof(T) > 12
             const int query = A.over_group((uint32_t)(t + r));
             return R.row(q0 + query, head_k * A.group + (t + r - query * A.group));
         };
-        tq.load(tid, n, A.D, [&](int r) { return at(A.q, r); });
-        tg.load(tid, n, A.D, [&](int r) { return at(A.go, r); });
+        tq.load_rows(tid, n, A.D, [&](int r) { return at(A.q, r); });
+        tg.load_rows(tid, n, A.D, [&](int r) { return at(A.go, r); });
         st = make_float4(0, 0, 0, INFINITY);        // rows behind the end: weight 0
         if (tid < n && tid < BN) {
             const int in_segment = A.over_group((uint32_t)(t + tid)), head = head_k * A.group + (t + tid - in_segment * A.group);

@@ -54,10 +54,12 @@ __global__ __launch_bounds__(64 * ROWW * KEYW, ROWW == 1 && DP * sizeof(T) > 128
     float top = -INFINITY, sum = 0;
     Transfer<M, DP, BN, F::STAGERS> tk, tv;
     PlaceTransfer<BN, F::STAGERS> tp;
+    tk.place(tid, A.k.token_bytes);
+    tv.place(tid, A.v.token_bytes);
     auto fetch = [&](int t) {
         const int n = end - t;
-        tk.load(tid, n, A.D, [&](int r) { return A.k.row(k0 + t + r, head_k); });
-        tv.load(tid, n, A.D, [&](int r) { return A.v.row(k0 + t + r, head_k); });
+        tk.load(A.k.row(k0 + t, head_k), tid, n, A.D);
+        tv.load(A.v.row(k0 + t, head_k), tid, n, A.D);
         if (A.score.biased) tp.load(tid, min(n, BN), A.k_pos + (int64_t)(k0 + t) * 3);
     };
     const int first = begin + keyw * BN;

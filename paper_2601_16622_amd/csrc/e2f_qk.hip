@@ -101,11 +101,14 @@ __global__ __launch_bounds__(THREADS) void k_qk(QkParams A) {
 #pragma unroll
         for (int u = 0; u < V; ++u) w[k][u] = e0 < A.D && A.w[k] ? A.w[k][e0 + u] : 1.0f;
     const int h0 = blockIdx.y * A.heads_per_wave, h1 = min(h0 + A.heads_per_wave, A.H[0] + A.H[1]);
+    auto row_of = [&](int hh) { return hh >= A.H[0] ? A.x[1].row(token, hh - A.H[0]) : A.x[0].row(token, hh); };
+    auto fetch = [&](int hh) { return in && hh < h1 ? *reinterpret_cast<const u32x4*>(row_of(hh) + e0 * sizeof(T)) : u32x4{0, 0, 0, 0}; };
+    u32x4 next = fetch(h0);
     for (int hh = h0; hh < h1; ++hh) {
         const int k = hh >= A.H[0], h = hh - (k ? A.H[0] : 0);
-        const char* row = A.x[k].row(token, h);
-        u32x4 raw = {0, 0, 0, 0};
-        if (in) raw = *reinterpret_cast<const u32x4*>(row + e0 * sizeof(T));
+        const char* row = row_of(hh);
+        const u32x4 raw = next;
+        next = fetch(hh + 1);
         float x[V], sum = 0.0f, t[V], y[V];
         Vec<T>::unpack(raw, x);
 #pragma unroll
@@ -140,14 +143,17 @@ __global__ __launch_bounds__(THREADS) void k_qk_bwd(QkParams A) {
         const bool in = token < A.N && e0 < A.D;
         float c[V], s[V];
         angles<V, P>(A, e0, A.rot && token < A.N ? A.position[token] : 0, c, s);
+        auto row_of = [&](const Rows (&R)[2], int hh) { return hh >= A.H[0] ? R[1].row(token, hh - A.H[0]) : R[0].row(token, hh); };
+        auto fetch = [&](const Rows (&R)[2], int hh) {
+            return in && hh < h1 ? *reinterpret_cast<const u32x4*>(row_of(R, hh) + e0 * sizeof(T)) : u32x4{0, 0, 0, 0};
+        };
+        u32x4 next = fetch(A.x, h0), gnext = fetch(A.dy, h0);
         for (int hh = h0; hh < h1; ++hh) {
             const int k = hh >= A.H[0], h = hh - (k ? A.H[0] : 0);
-            const char* grow = A.dy[k].row(token, h);
-            u32x4 raw = {0, 0, 0, 0}, graw = {0, 0, 0, 0};
-            if (in) {
-                raw = *reinterpret_cast<const u32x4*>(A.x[k].row(token, h) + e0 * sizeof(T));
-                graw = *reinterpret_cast<const u32x4*>(grow + e0 * sizeof(T));
-            }
+            const char* grow = row_of(A.dy, hh);
+            const u32x4 raw = next, graw = gnext;
+            next = fetch(A.x, hh + 1);
+            gnext = fetch(A.dy, hh + 1);
             float x[V], y[V], t[V], sum = 0.0f, dot = 0.0f;
             Vec<T>::unpack(raw, x);
             Vec<T>::unpack(graw, y);

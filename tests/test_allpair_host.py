@@ -79,7 +79,7 @@ def test_norm_refuses_bad_arguments(lib, kw, code):
 
 ROWS = [
     (heads(ptr=0), INVALID), (heads(token=-64), INVALID), (heads(head=-16), INVALID), (heads(ptr=fake + 4), UNSUPPORTED),
-    (heads(token=66), UNSUPPORTED), (heads(head=18), UNSUPPORTED), (heads(token=1 << 62), INVALID),
+    (heads(token=66), UNSUPPORTED), (heads(head=18), UNSUPPORTED), (heads(token=1 << 62), INVALID), (heads(token=1 << 23), UNSUPPORTED),
 ]
 RESULT_ROWS = ROWS + [(heads(token=0), INVALID), (heads(head=0), INVALID), (heads(token=16, head=16), INVALID), (heads(token=8), INVALID),
                       (heads(token=32, head=64), INVALID)]
