@@ -414,9 +414,10 @@ e2f_status e2f_qk_norm_rotate_backward(const e2f_qk_args *a, const e2f_heads *q,
  *                 are cut to 0 .. the segment's size
  *   q_pos, k_pos, slope   device float [Nq][3], [Nk][3], [Hq]; all three or none
  * Keys outside their segment's length and queries outside any segment's are not read.  A query without keys gets a zero row;
- * rows of out and of the gradients that no segment's length covers are left as they were.
+ * rows of out and of the gradients that no segment's length covers are left as they were.  No result may overlap an operand or
+ * another result.  A row's result is the same bits whatever the rows beside it hold.
  * Scores, softmax statistics and sums are binary32; with bf16 features the weights of the sum over v and the two factors of
- * the gradients' sums are rounded to bf16 for the matrix cores.
+ * the gradients' sums are rounded to bf16 for the matrix cores.  The gradients of slope and places take no such rounding.
  */
 typedef struct {
     int32_t dtype;          /* e2f_dtype of q, k, v, out and their gradients */
@@ -424,7 +425,7 @@ typedef struct {
     int32_t D;              /* features of a head, a multiple of 8, 8..128 */
     int32_t Nq, Nk, S;      /* query tokens, key tokens, segments */
     float scale;            /* finite */
-    float cap;              /* > 0, or 0 for none */
+    float cap;              /* 2^-20 .. 2^20, or 0 for none */
     const int32_t *q_offsets, *k_offsets, *q_lengths, *k_lengths;
     const float *q_pos, *k_pos, *slope;
 } e2f_dense_args;

@@ -370,6 +370,7 @@ def e2f_eaas_tensor_product(ctx, h, r, w_path, out):
 # sees pointers alone.  A refused tensor raises E2fError with E2F_ERR_INVALID_ARG; `where` names the call and the tensor.
 
 ROTARY = {"half": 0, "interleaved": 1}
+_INT32_MAX = 2 ** 31 - 1
 
 
 def _refuse(where):
@@ -437,6 +438,8 @@ def _qk_args(where, q, k, position=None, weight_q=None, weight_k=None, rotary_di
         _refuse(where)
     kind, device, f32 = _feature_type(x, where), x.device, torch.float32
     N, _, D = x.shape
+    if N > _INT32_MAX:
+        _refuse(where)
     Hq, Hk = 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
     a = QkArgs(kind, N, Hq, Hk, D, rotary_dim, ROTARY.get(layout, layout), eps, theta, position_scale,
                None if position is None else _plain(position, torch.int32, device, (N,), where, "position"),
@@ -486,6 +489,8 @@ def _dense_sizes(where, q, k, S):
     if k.dim() != 3:
         _refuse(f"{where}: k")
     (Nq, Hq, D), (Nk, Hk, _) = q.shape, k.shape
+    if max(Nq, Nk, S) > _INT32_MAX:
+        _refuse(where)
     return DenseArgs(kind, Hq, Hk, D, Nq, Nk, S, 1.0, 0.0)
 
 

@@ -20,7 +20,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 // What the score of a pair is formed from, in units of base-2 logarithms (so that the softmax's exponential is exp2).
 struct DenseScore {
     float in;            // x = in * (q . k): the argument of the tanh, or without a cap the score itself
-    float out, inv_out2; // cap log2(e) and its square's reciprocal
+    float out, inv_out;  // cap log2(e) and its reciprocal
     float c[8];          // odd polynomial of out * tanh
     int32_t capped, biased;
 };
@@ -355,8 +355,8 @@ __device__ __forceinline__ void cap_values(f32x16& p, f32x16& slack, const Dense
 #pragma unroll
         for (int k = 6; k >= 0; --k) t = t * y + A.c[k];
         if (SLACK) {
-            const float v = x * t;
-            slack[i] = 1.0f - v * A.inv_out2 * v;
+            const float v = x * t, th = v * A.inv_out;
+            slack[i] = 1.0f - th * th;
             p[i] = v - base;
         } else {
             p[i] = x * t - base;

@@ -318,6 +318,8 @@ e2f_status dense_check_sizes(const e2f_dense_args* a) {
         a->D <= 0 || a->Hq % a->Hk || !isfinite(a->scale) || !(a->cap >= 0.0f) || !isfinite(a->cap))
         return E2F_ERR_INVALID_ARG;
     if (a->D % 8 || a->D > 128 || a->Hq > 1024) return E2F_ERR_UNSUPPORTED;
+    // far from where the constants of the tanh leave binary32
+    if (a->cap > 0.0f && (a->cap < 0x1p-20f || a->cap > 0x1p20f)) return E2F_ERR_UNSUPPORTED;
     // the grid of either direction and the stacked rows of a segment are 31-bit numbers
     const int64_t most = INT32_MAX / a->Hk;
     if ((int64_t)a->Nq * (a->Hq / a->Hk) > INT32_MAX - 1024) return E2F_ERR_UNSUPPORTED;
@@ -364,7 +366,7 @@ void dense_fill(DenseParams& A, const e2f_dense_args* a, const e2f_heads* q, con
     s.in = s.capped ? a->scale / a->cap : (float)((double)a->scale * 1.4426950408889634);
     const double out = (double)a->cap * 1.4426950408889634;
     s.out = (float)out;
-    s.inv_out2 = s.capped ? (float)(1.0 / (out * out)) : 0.0f;
+    s.inv_out = s.capped ? (float)(1.0 / out) : 0.0f;
     // tanh x / x as a polynomial of x^2 on [0, 1], its relative error 4e-9 at most (minimised over the interval)
     static const double tanh_c[8] = {0.99999999577764732,   -0.33333278673333597, 0.13332159672365009,    -0.053870912721773931,
                                      0.021464820153790358, -0.0079174443902042118, 0.0022822293973515737, -0.00035334546706570396};

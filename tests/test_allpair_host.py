@@ -132,7 +132,7 @@ def dense(**kw):
 @pytest.mark.parametrize("kw,code", [
     (dict(dtype=5), INVALID), (dict(Nq=-1), INVALID), (dict(Nk=-1), INVALID), (dict(S=-1), INVALID), (dict(Hq=0), INVALID),
     (dict(Hk=0), INVALID), (dict(Hk=3), INVALID), (dict(D=0), INVALID), (dict(scale=float("nan")), INVALID), (dict(cap=-1.0), INVALID),
-    (dict(cap=float("nan")), INVALID), (dict(cap=float("inf")), INVALID), (dict(D=20), UNSUPPORTED), (dict(D=136), UNSUPPORTED),
+    (dict(cap=float("nan")), INVALID), (dict(cap=float("inf")), INVALID), (dict(cap=1e-7), UNSUPPORTED), (dict(cap=2e6), UNSUPPORTED), (dict(D=20), UNSUPPORTED), (dict(D=136), UNSUPPORTED),
     (dict(Hq=2048, Hk=1), UNSUPPORTED), (dict(q_offsets=None), INVALID), (dict(k_offsets=None), INVALID), (dict(slope=fake), INVALID),
     (dict(slope=fake, q_pos=fake), INVALID), (dict(q_pos=fake, k_pos=fake), INVALID), (dict(S=1 << 30, Hq=8, Hk=8), UNSUPPORTED),
 ])
