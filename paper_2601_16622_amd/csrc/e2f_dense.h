@@ -11,6 +11,8 @@
 // because the order in which a product's sum runs over the keys is free: operand V^T takes the keys in the order in which
 // the weights lie in the lanes.
 #pragma once
+#include <type_traits>
+
 #include "e2f_block.h"
 
 namespace e2f {
@@ -113,11 +115,13 @@ struct Mma;
 // bf16: v_mfma_f32_32x32x16_bf16, lane l: row l % 32, summands 8 (l/32) .. +7
 template <int DP>
 struct Mma<uint16_t, DP> {
-    using T = uint16_t;
+    using T = uint16_t;      // in memory
+    using E = uint16_t;      // in LDS
     // Rows are 16 banks of 64 apart (modulo 64), so that the transposed reads of 4 rows x 32 features meet no bank twice, and pieces
     // are exchanged within groups of four by the row, so that the reads of one piece of 8 rows do not either.
     static constexpr int STEPS = DP / 16, LD = DP == 64 ? 96 : DP == 128 ? 160 : DP;
     static __device__ __forceinline__ int piece(int row, int i) { return i ^ (row >> 2 & 3); }
+    static __device__ __forceinline__ void keep(E* tile, int row, int i, u32x4 x) { *reinterpret_cast<u32x4*>(tile + row * LD + piece(row, i) * 8) = x; }
     // a row of features as an operand, for products over the features
     struct Frag {
         bf16x8 x[STEPS];
@@ -167,34 +171,43 @@ struct Mma<uint16_t, DP> {
         for (int c = 0; c < 2; ++c) w.x[c] = __builtin_bit_cast(bf16x8, from[64 * c]);
         return w;
     }
-    // acc[dt] += (features 32 dt .. of the tile, transposed) W over the 32 tile rows from row0.  ds_read_b64_tr_b16 turns 4 rows of 16
-    // features in each 16 lanes: lane 4 r + c of them addresses features 4 c .. of row r, lane i gets feature i of the four rows.
-    template <int NT>
-    static __device__ __forceinline__ void accumulate(f32x16 (&acc)[NT], const T* tile, int row0, const Weights& w, int lane) {
+    // Transposed operands: ds_read_b64_tr_b16 turns 4 rows of 16 features in each 16 lanes: lane 4 r + c of them addresses features
+    // 4 c .. of row r, lane i gets feature i of the four rows.  p, q: a lane's places in rows 4 half .. and 8 + 4 half .., whose pieces
+    // are exchanged by half and 2 + half.
+    template <int LINE>
+    static __device__ __forceinline__ void turned_rows(const E* tile, int row0, int lane, const E*& p, const E*& q) {
+        const int half = lane >> 5, i = (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
+        const E* row = tile + (row0 + 4 * half + (lane >> 2 & 3)) * LINE + 4 * (lane & 1);
+        p = row + 8 * (i ^ half);
+        q = row + 8 * LINE + 8 * (i ^ (2 + half));
+    }
+    static __device__ __forceinline__ bf16x8 turned(const E* p, const E* q) {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4* lds4;
-        const int half = lane >> 5, i = (lane >> 4 & 1) * 2 + (lane >> 1 & 1);      // rows 4 half .. and 8 + 4 half ..: pieces by half and 2 + half
-        const T* row = tile + (row0 + 4 * half + (lane >> 2 & 3)) * LD + 4 * (lane & 1);
-        const T *p = row + 8 * (i ^ half), *q = row + 8 * LD + 8 * (i ^ (2 + half));
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)q);
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    // acc[dt] += (features 32 dt .. of the tile, transposed) W over the 32 tile rows from row0
+    template <int NT>
+    static __device__ __forceinline__ void accumulate(f32x16 (&acc)[NT], const E* tile, int row0, const Weights& w, int lane) {
+        const E *p, *q;
+        turned_rows<LD>(tile, row0, lane, p, q);
 #pragma unroll
         for (int dt = 0; dt < NT; ++dt)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + dt * 32 + 16 * c * LD));
-                const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(q + dt * 32 + 16 * c * LD));
-                const auto ab = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-                acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ab), w.x[c], acc[dt], 0, 0, 0);
-            }
+            for (int c = 0; c < 2; ++c)
+                acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned(p + dt * 32 + 16 * c * LD, q + dt * 32 + 16 * c * LD), w.x[c], acc[dt], 0, 0, 0);
     }
 };
 
-// binary32: v_mfma_f32_32x32x2_f32, lane l: row l % 32, summand l / 32.  The order of the sum over the features is free as
+// binary32 beyond 64 features: v_mfma_f32_32x32x2_f32, lane l: row l % 32, summand l / 32.  The order of the sum over the features is free as
 // well: the lower half of the lanes takes the first DP/2 features, so that a lane's operands lie side by side.
 template <int DP>
-struct Mma<float, DP> {
+struct MmaNative {
     using T = float;
+    using E = float;
     static constexpr int LD = DP + 8, H = DP / 2;
-    static __device__ __forceinline__ int piece(int, int i) { return i; }
+    static __device__ __forceinline__ void keep(E* tile, int row, int i, u32x4 x) { *reinterpret_cast<u32x4*>(tile + row * LD + i * 4) = x; }
     struct Frag {
         float x[H];
     };
@@ -252,6 +265,133 @@ struct Mma<float, DP> {
     }
 };
 
+// binary32 up to 64 features: a value as the sum of three bf16 with 8 bits of its significand each (cut, not rounded, so that the parts
+// keep its sign and are exact), a product as the six of nine partial products that are not below 2^-24 of it, each a bf16 matrix
+// instruction with binary32 sums.  For 16 summands these take 6 x 32 cycles where 8 binary32 instructions take 64 each.  (More
+// features would not leave room for the three parts of the operands in registers.)
+__device__ __forceinline__ void cut(float x, uint32_t (&part)[3]) {
+    part[0] = __float_as_uint(x);
+    const float r = x - __uint_as_float(part[0] & 0xFFFF0000u);
+    part[1] = __float_as_uint(r);
+    part[2] = __float_as_uint(r - __uint_as_float(part[1] & 0xFFFF0000u));
+}
+// the upper halves of two words, the first in the low half
+__device__ __forceinline__ uint32_t upper(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302); }
+
+template <int DP>
+struct MmaSplit {
+    using T = float;
+    using E = uint16_t;
+    using Row = Mma<uint16_t, DP>;
+    static constexpr int STEPS = DP / 16, LD = DP == 64 ? 224 : 96;      // a row's three parts one after the other, rows 48 banks apart
+    static_assert(DP == 32 || DP == 64, "");
+    static __device__ __forceinline__ void keep(E* tile, int row, int i, u32x4 x) {
+        uint32_t p[4][3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) cut(__uint_as_float(x[e]), p[e]);
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            *reinterpret_cast<u32x2*>(tile + row * LD + k * DP + Row::piece(row, i >> 1) * 8 + (i & 1) * 4) = u32x2{upper(p[0][k], p[1][k]), upper(p[2][k], p[3][k])};
+    }
+    struct Frag {
+        bf16x8 x[3][STEPS];
+    };
+    static __device__ __forceinline__ void cut8(const float (&f)[8], bf16x8 (&x)[3]) {
+        uint32_t p[8][3];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) cut(f[e], p[e]);
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            x[k] = __builtin_bit_cast(bf16x8, u32x4{upper(p[0][k], p[1][k]), upper(p[2][k], p[3][k]), upper(p[4][k], p[5][k]), upper(p[6][k], p[7][k])});
+    }
+    static __device__ __forceinline__ void load(Frag& f, const char* row, int D, bool valid, int half) {
+#pragma unroll
+        for (int c = 0; c < STEPS; ++c) {
+            const int d = 16 * c + 8 * half;
+            float x[8] = {};
+            if (valid && d < D) {
+                const f32x4 a = *reinterpret_cast<const f32x4*>(row + d * 4), b = *reinterpret_cast<const f32x4*>(row + d * 4 + 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = a[e];
+                    x[4 + e] = b[e];
+                }
+            }
+            bf16x8 parts[3];
+            cut8(x, parts);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) f.x[k][c] = parts[k];
+        }
+    }
+    // the small partial products first
+    static __device__ __forceinline__ f32x16 product(const bf16x8 (&a)[3], const bf16x8& b0, const bf16x8& b1, const bf16x8& b2, f32x16 acc) {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[2], b0, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1], b1, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b2, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1], b0, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b1, acc, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b0, acc, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 dot(const E* tile, int row0, const Frag& b, int lane) {
+        f32x16 acc = {};
+        const E* row = tile + (row0 + (lane & 31)) * LD;
+        const E* p[2] = {row + 8 * Row::piece(lane, lane >> 5), row + 8 * Row::piece(lane, 2 + (lane >> 5))};
+#pragma unroll
+        for (int c = 0; c < STEPS; ++c) {
+            bf16x8 a[3];
+#pragma unroll
+            for (int k = 0; k < 3; ++k) a[k] = *reinterpret_cast<const bf16x8*>(p[c & 1] + 32 * (c >> 1) + k * DP);
+            acc = product(a, b.x[0][c], b.x[1][c], b.x[2][c], acc);
+        }
+        return acc;
+    }
+    struct Weights {
+        bf16x8 x[3][2];
+    };
+    static __device__ __forceinline__ Weights weights(const f32x16& p) {
+        Weights w;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = p[8 * c + e];
+            bf16x8 parts[3];
+            cut8(f, parts);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) w.x[k][c] = parts[k];
+        }
+        return w;
+    }
+    static constexpr int WEIGHT_VECTORS = 6;
+    static __device__ __forceinline__ void put(u32x4* to, const Weights& w) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) to[64 * i] = __builtin_bit_cast(u32x4, w.x[i / 2][i % 2]);
+    }
+    static __device__ __forceinline__ Weights get(const u32x4* from) {
+        Weights w;
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w.x[i / 2][i % 2] = __builtin_bit_cast(bf16x8, from[64 * i]);
+        return w;
+    }
+    template <int NT>
+    static __device__ __forceinline__ void accumulate(f32x16 (&acc)[NT], const E* tile, int row0, const Weights& w, int lane) {
+        const E *p, *q;
+        Row::template turned_rows<LD>(tile, row0, lane, p, q);
+#pragma unroll
+        for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                bf16x8 a[3];
+#pragma unroll
+                for (int k = 0; k < 3; ++k) a[k] = Row::turned(p + dt * 32 + 16 * c * LD + k * DP, q + dt * 32 + 16 * c * LD + k * DP);
+                acc[dt] = product(a, w.x[0][c], w.x[1][c], w.x[2][c], acc[dt]);
+            }
+    }
+};
+
+template <int DP>
+struct Mma<float, DP> : std::conditional_t<(DP <= 64), MmaSplit<DP <= 64 ? DP : 64>, MmaNative<DP>> {};
+
 // BN rows of features on their way from memory into a tile, in the registers of THREADS threads: rows and features behind the end as zeros.
 // Rows at one stride (below 2^25 bytes): a load's address is the tile's, the same for all threads, and a 32-bit offset that a thread
 // forms once, so that the loop has no vector instructions for addresses (10 000 atoms 570 -> 560 us).  Rows of several heads: the row's.
@@ -291,11 +431,11 @@ struct Transfer {
             if (r < n && d < D) x[j] = *reinterpret_cast<const u32x4*>(row_at(r) + d * sizeof(T));
         }
     }
-    __device__ __forceinline__ void store(int tid, T* tile) const {
+    __device__ __forceinline__ void store(int tid, typename M::E* tile) const {
 #pragma unroll
         for (int j = 0; j < EACH; ++j) {
-            const int i = tid + j * THREADS, r = i / VECS;
-            *reinterpret_cast<u32x4*>(tile + r * M::LD + M::piece(r, i % VECS) * V) = x[j];
+            const int i = tid + j * THREADS;
+            M::keep(tile, i / VECS, i % VECS, x[j]);
         }
     }
 };

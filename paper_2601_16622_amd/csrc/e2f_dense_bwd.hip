@@ -31,10 +31,10 @@ struct RowWalk {
     using M = Mma<T, DP>;
     static constexpr int BN = SHARE > 1 ? 32 * SHARE : ROWW > 1 && sizeof(T) == 2 ? 64 : 32, BM = 32 * ROWW, THREADS = 64 * ROWW * SHARE;
     struct Tile {
-        T k[BN * M::LD], v[BN * M::LD];
+        typename M::E k[BN * M::LD], v[BN * M::LD];
         float place[3 * BN];
     };
-    int lane, half, group, share, head_k, k0, begin, end, query, head, first_head;
+    int lane, half, group, share, head_k, k0, nk, begin, end, query, head, first_head;
     int64_t at;            // of the row among [Nq][Hq]
     bool any, valid, busy;
     float x, y, z, slope;
@@ -48,8 +48,9 @@ struct RowWalk {
         head_k = blockIdx.x % A.Hk;
         const int64_t tile = blockIdx.x / A.Hk;
         const Segment segment = segment_of<false>(A, BM, tile);
-        const int q0 = segment.q0, nq = segment.nq, nk = segment.nk;
+        const int q0 = segment.q0, nq = segment.nq;
         k0 = segment.k0;
+        nk = segment.nk;
         const int64_t row0 = (tile - segment.first) * BM, rows = (int64_t)nq * A.group;
         any = row0 >= 0 && row0 < rows;
         if (!any) return;
@@ -192,6 +193,17 @@ __global__ __launch_bounds__(64 * ROWW * SHARE, ROWW == 1 && DP * sizeof(T) > 12
     const float top = st.x, inv = st.y, delta = st.z, slope2 = w.slope * LOG2E;
     // weights stay without 1 / sum: a row's sums get it at the end
     float dslope = 0, gx = 0, gy = 0, gz = 0;
+    // a row's ds sum up to nothing, so that any distance may be taken off all of its distances: with one of about their size the sum
+    // of ds d cancels less, and the rounding of delta counts less in it
+    float usual = 0;
+    if (A.score.biased && w.nk > 0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {      // the mean over 16 keys across the segment
+            const float* at = A.k_pos + (w.k0 + (int64_t)w.nk * i / 16) * 3;
+            const float dx = w.x - at[0], dy = w.y - at[1], dz = w.z - at[2];
+            usual += 0.0625f * __builtin_amdgcn_sqrtf(dx * dx + dy * dy + dz * dz);
+        }
+    }
     f32x16 acc[NT] = {};
     auto weigh = [&](int m, int n) {
         f32x16 p = M::dot(tile.k, m, w.qf, w.lane), slack;
@@ -212,7 +224,7 @@ __global__ __launch_bounds__(64 * ROWW * SHARE, ROWW == 1 && DP * sizeof(T) > 12
                     float d, id;
                     distance(dx, dy, dz, d, id);
                     p[i] = __builtin_amdgcn_exp2f(p[i] - slope2 * d) * (dp[i] - delta);
-                    ts += p[i] * d;
+                    ts += p[i] * (d - usual);
                     const float f = p[i] * id;
                     tx += f * dx;
                     ty += f * dy;
@@ -307,8 +319,8 @@ __global__ __launch_bounds__(64 * KEYW * SHARE, KEYW == 1 && DP * sizeof(T) > 12
     using M = Mma<T, DP>;
     constexpr int BN = SHARE > 1 ? 32 * SHARE : KEYW > 1 && sizeof(T) == 2 ? 64 : 32, BM = 32 * KEYW, THREADS = 64 * KEYW * SHARE;
     constexpr int NT = DP / SHARE / 32;
-    __shared__ __align__(16) T qs[BN * M::LD];
-    __shared__ __align__(16) T gs[BN * M::LD];
+    __shared__ __align__(16) typename M::E qs[BN * M::LD];
+    __shared__ __align__(16) typename M::E gs[BN * M::LD];
     __shared__ __align__(16) float par[ROW_LINES][BN];
     __shared__ __align__(16) u32x4 passed[SHARE > 1 ? KEYW * SHARE : 1][2][SHARE > 1 ? M::WEIGHT_VECTORS * 64 : 1];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = (tid >> 6) % KEYW, share = (tid >> 6) / KEYW;
@@ -545,7 +557,7 @@ __global__ __launch_bounds__(SUM_THREADS) void k_dense_bwd_join(Rows out, const 
 }
 
 // Workgroups of 128 rows (keys), or of 32 where a segment has no more than 64 of them on average; and parts of the other side
-// where the workgroups do not fill the chip evenly: two of four waves to a compute unit, or one of eight with more than 64 features.
+// where the workgroups do not fill the chip evenly: two of four waves to a compute unit, or one of eight.
 struct BwdPlan {
     int row_waves, key_waves, stat_parts, row_parts, key_parts;
     int64_t row_tiles, key_tiles;
@@ -563,13 +575,13 @@ BwdPlan bwd_plan(const e2f_dense_args* a) {
     // 128 features, 314 workgroups over rows take 475 us in one part, 401 in three and 387 in four; 80 over keys, 20 012 rows, take
     // 1 600 us in one part and 533 in twelve as in three
     const double step = a->dtype == E2F_BF16 ? 0.03 + 0.0004 * a->D : 0.05 + 0.004 * a->D;
-    const int slots = a->D > 64 ? 256 : 512;
+    const int row_slots = a->D > 64 ? 256 : 512, key_slots = a->D * elem_bytes(a->dtype) > 128 ? 256 : 512;
     if (P.row_tiles) {
         const int64_t blocks = P.row_tiles * a->Hk * P.row_waves / 4 + 1, most = a->Nk / S / 256;
         P.stat_parts = best_parts(blocks, 512, a->Nk / S * step, rows * a->Hk * 32.0 / 4.5e6, most);
-        P.row_parts = best_parts(blocks, slots, a->Nk / S * step, rows * a->Hk * a->D * 8.0 / 4.5e6, most);
+        P.row_parts = best_parts(blocks, row_slots, a->Nk / S * step, rows * a->Hk * a->D * 8.0 / 4.5e6, most);
     }
-    if (P.key_tiles) P.key_parts = best_parts(P.key_tiles * a->Hk * P.key_waves / 4 + 1, slots, rows / S * step, (double)a->Nk * a->Hk * a->D * 16.0 / 4.5e6, rows / S / 256);
+    if (P.key_tiles) P.key_parts = best_parts(P.key_tiles * a->Hk * P.key_waves / 4 + 1, key_slots, rows / S * step, (double)a->Nk * a->Hk * a->D * 16.0 / 4.5e6, rows / S / 256);
     return P;
 }
 
@@ -578,8 +590,9 @@ void launch_dp(const DenseParams& A, const BwdPlan& P, hipStream_t st) {
     const dim3 stats((unsigned)(P.row_tiles * A.Hk), (unsigned)P.stat_parts), rows(stats.x, (unsigned)P.row_parts),
         keys((unsigned)(P.key_tiles * A.Hk), (unsigned)P.key_parts);
     const int64_t n = (int64_t)A.Nq * A.Hk * A.group;
-    // more than 64 features: two waves to a group of rows or keys
-    constexpr int KD = DP > 64 ? 128 : DP, SHARE = DP > 64 ? 2 : 1;
+    // more than 64 features: two waves to a group of rows or keys; of keys also beyond 32 features in fp32 (48 features, 4 x 1 000 atoms: rows
+    // 215 us with two waves and 199 with one, keys 196 and 245)
+    constexpr int KD = DP > 64 ? 128 : DP, SHARE = DP > 64 ? 2 : 1, KEY_SHARE = DP * sizeof(T) > 128 ? 2 : 1;
     if (rows.x) {
         if (P.row_waves == 4) k_dense_bwd_stats<T, DP, 4><<<stats, 256, 0, st>>>(A);
         else k_dense_bwd_stats<T, DP, 1><<<stats, 64, 0, st>>>(A);
@@ -590,8 +603,8 @@ void launch_dp(const DenseParams& A, const BwdPlan& P, hipStream_t st) {
     if (keys.x) {
         auto go = [&](auto cap, auto bias) {
             constexpr bool CAP = decltype(cap)::value, BIAS = decltype(bias)::value;
-            if (P.key_waves == 4) k_dense_bwd_keys<T, KD, 4, SHARE, CAP, BIAS><<<keys, 256 * SHARE, 0, st>>>(A);
-            else k_dense_bwd_keys<T, KD, 1, SHARE, CAP, BIAS><<<keys, 64 * SHARE, 0, st>>>(A);
+            if (P.key_waves == 4) k_dense_bwd_keys<T, KD, 4, KEY_SHARE, CAP, BIAS><<<keys, 256 * KEY_SHARE, 0, st>>>(A);
+            else k_dense_bwd_keys<T, KD, 1, KEY_SHARE, CAP, BIAS><<<keys, 64 * KEY_SHARE, 0, st>>>(A);
         };
         const std::true_type yes;
         const std::false_type no;

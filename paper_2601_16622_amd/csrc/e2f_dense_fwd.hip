@@ -13,7 +13,7 @@ struct FwdShape {
     using M = Mma<T, DP>;
     static constexpr int BN = ROWW > 1 && sizeof(T) == 2 ? 64 : 32, BM = 32 * ROWW, THREADS = 64 * ROWW * KEYW, STAGERS = 64 * ROWW;
     struct Tile {
-        T k[BN * M::LD], v[BN * M::LD];
+        typename M::E k[BN * M::LD], v[BN * M::LD];
         float place[3 * BN];
     };
 };
