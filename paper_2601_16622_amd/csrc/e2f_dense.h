@@ -38,6 +38,7 @@ struct DenseParams {
     DenseScore score;
     float *part, *part_sum;        // forward with split keys: [splits][Nq][Hq][D] sums over a part's keys, [splits][Nq][Hq][2] reference, sum
     float4* stats;                 // backward: [Nq][Hq] softmax reference, 1 / sum, delta, reference + log2(sum)
+    float* usual;                  // backward: [Nq][Hq] mean distance under a row's weights
     // of the parts of a backward pass: [parts] of [row tiles][Hq], [Hq][Nq][3], [Hk][Nk][3], [Nq][Hq], [Nq][Hq][D], [Nk][Hk][D]
     float *slope_part, *q_pos_part, *k_pos_part;
     float4* stats_part;
@@ -559,18 +560,28 @@ __device__ __forceinline__ bool move_reference(f32x16& p, float& top, float& shr
     return true;
 }
 
-// p -= slope * distance; the places of the tile's rows lie in three lines of BN, `at` the lane's first row.
+// Distances of a lane's row to the tile's keys `at` .. `at` + 3, whose places lie in three lines of BN.
+template <int BN>
+__device__ __forceinline__ f32x4 key_distances(float x, float y, float z, const float* place, int at) {
+    const f32x4 px = *reinterpret_cast<const f32x4*>(place + at), py = *reinterpret_cast<const f32x4*>(place + BN + at),
+                pz = *reinterpret_cast<const f32x4*>(place + 2 * BN + at);
+    f32x4 d;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float dx = x - px[e], dy = y - py[e], dz = z - pz[e];
+        d[e] = __builtin_amdgcn_sqrtf(dx * dx + dy * dy + dz * dz);
+    }
+    return d;
+}
+
+// p -= slope * distance; `at`: the lane's first key.
 template <int BN>
 __device__ __forceinline__ void bias_scores(f32x16& p, float x, float y, float z, float slope, const float* place, int at) {
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-        const f32x4 px = *reinterpret_cast<const f32x4*>(place + at + 8 * b), py = *reinterpret_cast<const f32x4*>(place + BN + at + 8 * b),
-                    pz = *reinterpret_cast<const f32x4*>(place + 2 * BN + at + 8 * b);
+        const f32x4 d = key_distances<BN>(x, y, z, place, at + 8 * b);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float dx = x - px[e], dy = y - py[e], dz = z - pz[e];
-            p[4 * b + e] -= slope * __builtin_amdgcn_sqrtf(dx * dx + dy * dy + dz * dz);
-        }
+        for (int e = 0; e < 4; ++e) p[4 * b + e] -= slope * d[e];
     }
 }
 

@@ -34,7 +34,7 @@ struct RowWalk {
         typename M::E k[BN * M::LD], v[BN * M::LD];
         float place[3 * BN];
     };
-    int lane, half, group, share, head_k, k0, nk, begin, end, query, head, first_head;
+    int lane, half, group, share, head_k, k0, begin, end, query, head, first_head;
     int64_t at;            // of the row among [Nq][Hq]
     bool any, valid, busy;
     float x, y, z, slope;
@@ -48,9 +48,8 @@ struct RowWalk {
         head_k = blockIdx.x % A.Hk;
         const int64_t tile = blockIdx.x / A.Hk;
         const Segment segment = segment_of<false>(A, BM, tile);
-        const int q0 = segment.q0, nq = segment.nq;
+        const int q0 = segment.q0, nq = segment.nq, nk = segment.nk;
         k0 = segment.k0;
-        nk = segment.nk;
         const int64_t row0 = (tile - segment.first) * BM, rows = (int64_t)nq * A.group;
         any = row0 >= 0 && row0 < rows;
         if (!any) return;
@@ -115,7 +114,7 @@ struct RowWalk {
     }
 };
 
-// Softmax statistics of the rows: reference, sum, sum of p dp.  With parts of the keys each leaves its own, [parts][Nq][Hq].
+// Softmax statistics of the rows: reference, sum, sum of p dp, sum of p d.  With parts of the keys each leaves its own, [parts][Nq][Hq].
 template <typename T, int DP, int ROWW>
 __global__ __launch_bounds__(64 * ROWW, ROWW == 1 && DP * sizeof(T) > 256 ? 1 : 2) void k_dense_bwd_stats(DenseParams A) {
     using R = RowWalk<T, DP, ROWW, 1>;
@@ -123,36 +122,54 @@ __global__ __launch_bounds__(64 * ROWW, ROWW == 1 && DP * sizeof(T) > 256 ? 1 : 
     __shared__ __align__(16) typename R::Tile tile;
     R w(A);
     if (!w.any) return;
-    float top = -INFINITY, sum = 0, delta = 0;
+    float top = -INFINITY, sum = 0, delta = 0, usual = 0;
     w.walk(A, tile, [&](int m, int n) {
-        f32x16 p = M::dot(tile.k, m, w.qf, w.lane);
+        f32x16 p = M::dot(tile.k, m, w.qf, w.lane), d;
         const f32x16 dp = M::dot(tile.v, m, w.gf, w.lane);
         cap_scores<false>(p, p, A.score, reference_base(top));
-        if (A.score.biased) bias_scores<R::BN>(p, w.x, w.y, w.z, w.slope * LOG2E, tile.place, m + 4 * w.half);
+        if (A.score.biased) {
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const f32x4 of = key_distances<R::BN>(w.x, w.y, w.z, tile.place, m + 4 * w.half + 8 * b);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    d[4 * b + e] = of[e];
+                    p[4 * b + e] -= w.slope * LOG2E * of[e];
+                }
+            }
+        }
         w.mask(p, n);
         float shrink;
         if (move_reference(p, top, shrink)) {
             sum *= shrink;
             delta *= shrink;
+            usual *= shrink;
         }
-        float add = 0, dot = 0;
+        float add = 0, dot = 0, far = 0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const float e = __builtin_amdgcn_exp2f(p[i]);
-            add += e;
-            dot += e * dp[i];
+            p[i] = __builtin_amdgcn_exp2f(p[i]);
+            add += p[i];
+            dot += p[i] * dp[i];
+        }
+        if (A.score.biased) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) far += p[i] * d[i];
         }
         sum += add;
         delta += dot;
+        usual += far;
     });
     sum += other_half(sum);
     delta += other_half(delta);
+    usual += other_half(usual);
     if (!w.valid || w.half) return;
     if (gridDim.y == 1) {
         const float inv = w.begin < w.end ? 1.0f / sum : 0.0f;
         A.stats[w.at] = make_float4(top, inv, delta * inv, top - __builtin_amdgcn_logf(inv));
+        if (A.score.biased) A.usual[w.at] = usual * inv;
     } else {
-        A.stats_part[(int64_t)blockIdx.y * A.Nq * (A.Hk * A.group) + w.at] = make_float4(top, sum, delta, 0.0f);
+        A.stats_part[(int64_t)blockIdx.y * A.Nq * (A.Hk * A.group) + w.at] = make_float4(top, sum, delta, usual);
     }
 }
 
@@ -160,16 +177,18 @@ __global__ __launch_bounds__(64 * ROWW, ROWW == 1 && DP * sizeof(T) > 256 ? 1 : 
 __global__ __launch_bounds__(SUM_THREADS) void k_dense_bwd_join_stats(DenseParams A, int parts) {
     const int64_t rows = (int64_t)A.Nq * (A.Hk * A.group), row = (int64_t)blockIdx.x * SUM_THREADS + threadIdx.x;
     if (row >= rows) return;
-    float top = -INFINITY, sum = 0, delta = 0;
+    float top = -INFINITY, sum = 0, delta = 0, usual = 0;
     for (int p = 0; p < parts; ++p) top = fmaxf(top, A.stats_part[p * rows + row].x);
     for (int p = 0; p < parts; ++p) {
         const float4 s = A.stats_part[p * rows + row];
         const float f = top > -INFINITY ? __builtin_amdgcn_exp2f(s.x - top) : 1.0f;
         sum += f * s.y;
         delta += f * s.z;
+        usual += f * s.w;
     }
     const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;      // no keys: no weights
     A.stats[row] = make_float4(top, inv, delta * inv, top - __builtin_amdgcn_logf(inv));
+    if (A.score.biased) A.usual[row] = usual * inv;
 }
 
 // dq and a row's shares of the gradients of slope and place, from the statistics.  SHARE waves to a group of rows pass each other the
@@ -193,17 +212,9 @@ __global__ __launch_bounds__(64 * ROWW * SHARE, ROWW == 1 && DP * sizeof(T) > 12
     const float top = st.x, inv = st.y, delta = st.z, slope2 = w.slope * LOG2E;
     // weights stay without 1 / sum: a row's sums get it at the end
     float dslope = 0, gx = 0, gy = 0, gz = 0;
-    // a row's ds sum up to nothing, so that any distance may be taken off all of its distances: with one of about their size the sum
-    // of ds d cancels less, and the rounding of delta counts less in it
-    float usual = 0;
-    if (A.score.biased && w.nk > 0) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {      // the mean over 16 keys across the segment
-            const float* at = A.k_pos + (w.k0 + (int64_t)w.nk * i / 16) * 3;
-            const float dx = w.x - at[0], dy = w.y - at[1], dz = w.z - at[2];
-            usual += 0.0625f * __builtin_amdgcn_sqrtf(dx * dx + dy * dy + dz * dz);
-        }
-    }
+    // a row's ds sum up to nothing, so that any distance may be taken off all of its distances: with the mean distance under the row's
+    // weights the rounding of delta, a multiple of those weights in ds, drops out of the sum of ds d
+    const float usual = A.score.biased ? A.usual[w.at] : 0.0f;
     f32x16 acc[NT] = {};
     auto weigh = [&](int m, int n) {
         f32x16 p = M::dot(tile.k, m, w.qf, w.lane), slack;
@@ -641,6 +652,7 @@ size_t layout(const e2f_dense_args* a, const BwdPlan& P, char* ws, DenseParams* 
     };
     const size_t rows = (size_t)a->Nq * a->Hq, keys = (size_t)a->Nk * a->Hk, sp = P.stat_parts, rp = P.row_parts, kp = P.key_parts;
     float* stats = take(rows * 4);
+    float* usual = take(a->slope ? rows : 0);
     float* slope = take(a->slope ? rp * P.row_tiles * a->Hq : 0);
     float* qp = take(a->slope ? rp * rows * 3 : 0);
     float* kpos = take(a->slope ? kp * keys * 3 : 0);
@@ -650,6 +662,7 @@ size_t layout(const e2f_dense_args* a, const BwdPlan& P, char* ws, DenseParams* 
     float* gv = take(kp > 1 ? kp * keys * a->D : 0);
     if (A) {
         A->stats = reinterpret_cast<float4*>(stats);
+        A->usual = usual;
         A->slope_part = slope;
         A->q_pos_part = qp;
         A->k_pos_part = kpos;
