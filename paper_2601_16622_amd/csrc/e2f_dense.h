@@ -108,6 +108,9 @@ __device__ __forceinline__ int token_segment(const int32_t* offsets, int S, int 
 
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
 
+// the upper halves of two words, the first in the low half
+__device__ __forceinline__ uint32_t upper(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302); }
+
 // Matrix instructions and operands of the two feature types.  DP: D rounded up to 32, zero beyond D.  A tile is BN rows of
 // features in LDS, LD elements from row to row, a row's 16-byte pieces in the order piece(row, .).
 template <typename T, int DP>
@@ -172,6 +175,33 @@ struct Mma<uint16_t, DP> {
         for (int c = 0; c < 2; ++c) w.x[c] = __builtin_bit_cast(bf16x8, from[64 * c]);
         return w;
     }
+    // weights as the sum of two bf16 (the first cut, the second what is left, rounded: 16 bits), for sums whose terms cancel
+    struct Fine {
+        Weights w[2];
+    };
+    static __device__ __forceinline__ Fine fine(const f32x16& p) {
+        Fine f;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            u32x4 x, y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float a = p[8 * c + 2 * e], b = p[8 * c + 2 * e + 1];
+                const uint32_t i = __float_as_uint(a), j = __float_as_uint(b);
+                x[e] = upper(i, j);
+                y[e] = pack_bf16(a - __uint_as_float(i & 0xFFFF0000u), b - __uint_as_float(j & 0xFFFF0000u));
+            }
+            f.w[0].x[c] = __builtin_bit_cast(bf16x8, x);
+            f.w[1].x[c] = __builtin_bit_cast(bf16x8, y);
+        }
+        return f;
+    }
+    static constexpr int FINE_VECTORS = 4;
+    static __device__ __forceinline__ void put(u32x4* to, const Fine& f) {
+        put(to, f.w[0]);
+        put(to + 128, f.w[1]);
+    }
+    static __device__ __forceinline__ Fine get_fine(const u32x4* from) { return Fine{{get(from), get(from + 128)}}; }
     // Transposed operands: ds_read_b64_tr_b16 turns 4 rows of 16 features in each 16 lanes: lane 4 r + c of them addresses features
     // 4 c .. of row r, lane i gets feature i of the four rows.  p, q: a lane's places in rows 4 half .. and 8 + 4 half .., whose pieces
     // are exchanged by half and 2 + half.
@@ -198,6 +228,19 @@ struct Mma<uint16_t, DP> {
 #pragma unroll
             for (int c = 0; c < 2; ++c)
                 acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned(p + dt * 32 + 16 * c * LD, q + dt * 32 + 16 * c * LD), w.x[c], acc[dt], 0, 0, 0);
+    }
+    template <int NT>
+    static __device__ __forceinline__ void accumulate(f32x16 (&acc)[NT], const E* tile, int row0, const Fine& f, int lane) {
+        const E *p, *q;
+        turned_rows<LD>(tile, row0, lane, p, q);
+#pragma unroll
+        for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const bf16x8 a = turned(p + dt * 32 + 16 * c * LD, q + dt * 32 + 16 * c * LD);
+                acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, f.w[1].x[c], acc[dt], 0, 0, 0);
+                acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, f.w[0].x[c], acc[dt], 0, 0, 0);
+            }
     }
 };
 
@@ -237,6 +280,9 @@ struct MmaNative {
         f32x16 x;
     };
     static __device__ __forceinline__ Weights weights(const f32x16& p) { return Weights{p}; }
+    static __device__ __forceinline__ Weights fine(const f32x16& p) { return Weights{p}; }
+    static constexpr int FINE_VECTORS = 4;
+    static __device__ __forceinline__ Weights get_fine(const u32x4* from) { return get(from); }
     static constexpr int WEIGHT_VECTORS = 4;
     static __device__ __forceinline__ void put(u32x4* to, const Weights& w) {
 #pragma unroll
@@ -276,9 +322,6 @@ __device__ __forceinline__ void cut(float x, uint32_t (&part)[3]) {
     part[1] = __float_as_uint(r);
     part[2] = __float_as_uint(r - __uint_as_float(part[1] & 0xFFFF0000u));
 }
-// the upper halves of two words, the first in the low half
-__device__ __forceinline__ uint32_t upper(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302); }
-
 template <int DP>
 struct MmaSplit {
     using T = float;
@@ -363,7 +406,9 @@ struct MmaSplit {
         }
         return w;
     }
-    static constexpr int WEIGHT_VECTORS = 6;
+    static __device__ __forceinline__ Weights fine(const f32x16& p) { return weights(p); }
+    static __device__ __forceinline__ Weights get_fine(const u32x4* from) { return get(from); }
+    static constexpr int WEIGHT_VECTORS = 6, FINE_VECTORS = 6;
     static __device__ __forceinline__ void put(u32x4* to, const Weights& w) {
 #pragma unroll
         for (int i = 0; i < 6; ++i) to[64 * i] = __builtin_bit_cast(u32x4, w.x[i / 2][i % 2]);

@@ -191,7 +191,8 @@ __global__ __launch_bounds__(SUM_THREADS) void k_dense_bwd_join_stats(DenseParam
     if (A.score.biased) A.usual[row] = usual * inv;
 }
 
-// dq and a row's shares of the gradients of slope and place, from the statistics.  SHARE waves to a group of rows pass each other the
+// dq and a row's shares of the gradients of slope and place, from the statistics.  In bf16 the factors of the sum over k are two bf16 each: a
+// row's factors sum up to nothing, and what the rounding of one leaves of dq would come close to twice its own rounding's share.  SHARE waves to a group of rows pass each other the
 // weights and keep the sums of DP / SHARE features each, as in the kernel over keys.
 template <typename T, int DP, int ROWW, int SHARE>
 __global__ __launch_bounds__(64 * ROWW * SHARE, ROWW == 1 && DP * sizeof(T) > 128 ? 1 : 2) void k_dense_bwd_rows(DenseParams A) {
@@ -199,7 +200,7 @@ __global__ __launch_bounds__(64 * ROWW * SHARE, ROWW == 1 && DP * sizeof(T) > 12
     using M = typename R::M;
     constexpr int BN = R::BN, NT = DP / SHARE / 32;
     __shared__ __align__(16) typename R::Tile tile;
-    __shared__ __align__(16) u32x4 passed[SHARE > 1 ? ROWW * SHARE : 1][SHARE > 1 ? M::WEIGHT_VECTORS * 64 : 1];
+    __shared__ __align__(16) u32x4 passed[SHARE > 1 ? ROWW * SHARE : 1][SHARE > 1 ? M::FINE_VECTORS * 64 : 1];
     R w(A);
     const int Hq = A.Hk * A.group;
     float* slopes = A.slope_part ? A.slope_part + ((int64_t)blockIdx.y * (gridDim.x / A.Hk) + blockIdx.x / A.Hk) * Hq + w.head_k * A.group : nullptr;
@@ -254,7 +255,7 @@ __global__ __launch_bounds__(64 * ROWW * SHARE, ROWW == 1 && DP * sizeof(T) > 12
 #pragma unroll
             for (int i = 0; i < 16; ++i) p[i] *= slack[i];
         }
-        return M::weights(p);
+        return M::fine(p);
     };
     if constexpr (SHARE == 1) {
         w.walk(A, tile, [&](int m, int n) { M::accumulate(acc, tile.k, m, weigh(m, n), w.lane); });
@@ -265,7 +266,7 @@ __global__ __launch_bounds__(64 * ROWW * SHARE, ROWW == 1 && DP * sizeof(T) > 12
             if (w.busy) {
 #pragma unroll
                 for (int u = 0; u < SHARE; ++u)
-                    M::accumulate(acc, tile.k + w.share * NT * 32, 32 * u, M::get(&passed[u * ROWW + w.group][w.lane]), w.lane);
+                    M::accumulate(acc, tile.k + w.share * NT * 32, 32 * u, M::get_fine(&passed[u * ROWW + w.group][w.lane]), w.lane);
             }
         });
     }

