@@ -696,6 +696,7 @@ e2f_status e2f_dense_attn_backward(const e2f_dense_args* a, const e2f_heads* q, 
         (rc = check_result_rows(grad_v, a->dtype, a->Nk, a->Hk, a->D)) != E2F_OK)
         return rc;
     if ((grad_slope || grad_q_pos || grad_k_pos) && !a->slope) return E2F_ERR_INVALID_ARG;
+    if (!word_aligned(grad_slope) || !word_aligned(grad_q_pos) || !word_aligned(grad_k_pos)) return E2F_ERR_INVALID_ARG;
     const BwdPlan P = bwd_plan(a);
     const size_t need = layout(a, P, nullptr, nullptr);
     if (need && (!ws || !aligned_ws(ws))) return E2F_ERR_INVALID_ARG;

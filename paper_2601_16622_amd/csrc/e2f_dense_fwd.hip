@@ -1,4 +1,6 @@
 // Attention among all atoms of a segment, forward: one pass over the keys with the running maximum and sum of the softmax.
+#include <initializer_list>
+
 #include "e2f_dense_api.h"
 
 namespace {
@@ -333,6 +335,9 @@ e2f_status dense_check(const e2f_dense_args* a) {
     if (rc != E2F_OK) return rc;
     if (a->slope ? (a->Nq > 0 && !a->q_pos) || (a->Nk > 0 && !a->k_pos) : a->q_pos || a->k_pos) return E2F_ERR_INVALID_ARG;
     if (a->S > 0 && (!a->q_offsets || !a->k_offsets)) return E2F_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)a->q_offsets, (const void*)a->k_offsets, (const void*)a->q_lengths, (const void*)a->k_lengths,
+                          (const void*)a->q_pos, (const void*)a->k_pos, (const void*)a->slope})
+        if (!word_aligned(p)) return E2F_ERR_INVALID_ARG;
     return E2F_OK;
 }
 

@@ -230,6 +230,7 @@ e2f_status check(const e2f_qk_args* a) {
         return E2F_ERR_INVALID_ARG;
     if (a->D % 8 || a->D > MAX_D || a->Hq > 1024 || a->Hk > 1024) return E2F_ERR_UNSUPPORTED;
     if (a->N > 0 && a->rotary_dim > 0 && !a->position) return E2F_ERR_INVALID_ARG;
+    if (!word_aligned(a->position) || !word_aligned(a->weight_q) || !word_aligned(a->weight_k)) return E2F_ERR_INVALID_ARG;
     return E2F_OK;
 }
 
@@ -360,6 +361,7 @@ e2f_status e2f_qk_norm_rotate_backward(const e2f_qk_args* a, const e2f_heads* q,
         return rc;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const bool empty = a->N == 0 || a->Hq + a->Hk == 0, sums = grad_weight_q || grad_weight_k;
+    if (!word_aligned(grad_weight_q) || !word_aligned(grad_weight_k)) return E2F_ERR_INVALID_ARG;
     const size_t need = e2f_qk_norm_rotate_backward_workspace_bytes(a);
     if (need && (!ws || !aligned_ws(ws))) return E2F_ERR_INVALID_ARG;
     if (ws_bytes < need) return E2F_ERR_WORKSPACE_TOO_SMALL;

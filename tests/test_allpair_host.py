@@ -68,13 +68,13 @@ def qk(**kw):
     (dict(rotary_dim=18), INVALID), (dict(rotary_dim=-2), INVALID), (dict(layout=2), INVALID), (dict(eps=0.0), INVALID),
     (dict(eps=float("nan")), INVALID), (dict(theta=0.0), INVALID), (dict(theta=float("inf")), INVALID),
     (dict(position_scale=float("inf")), INVALID), (dict(position=None), INVALID), (dict(D=12, rotary_dim=0), UNSUPPORTED),
-    (dict(D=264), UNSUPPORTED), (dict(Hk=1025), UNSUPPORTED),
+    (dict(D=264), UNSUPPORTED), (dict(Hk=1025), UNSUPPORTED), (dict(position=fake + 2), INVALID), (dict(weight_q=fake + 1), INVALID),
 ])
 def test_norm_refuses_bad_arguments(lib, kw, code):
     h = heads(token=1 << 14, head=264)
     assert lib.e2f_qk_norm_rotate(qk(**kw), h, h, h, h, None) == code
     assert lib.e2f_qk_norm_rotate_backward(qk(**kw), h, h, h, h, h, h, None, None, fake, 1 << 30, None) == code
-    assert kw.get("position", fake) is None or lib.e2f_qk_norm_rotate_backward_workspace_bytes(qk(**kw)) == 0
+    assert {"position", "weight_q"} & set(kw) or lib.e2f_qk_norm_rotate_backward_workspace_bytes(qk(**kw)) == 0
 
 
 ROWS = [
@@ -135,6 +135,7 @@ def dense(**kw):
     (dict(cap=float("nan")), INVALID), (dict(cap=float("inf")), INVALID), (dict(cap=1e-7), UNSUPPORTED), (dict(cap=2e6), UNSUPPORTED), (dict(D=20), UNSUPPORTED), (dict(D=136), UNSUPPORTED),
     (dict(Hq=2048, Hk=1), UNSUPPORTED), (dict(q_offsets=None), INVALID), (dict(k_offsets=None), INVALID), (dict(slope=fake), INVALID),
     (dict(slope=fake, q_pos=fake), INVALID), (dict(q_pos=fake, k_pos=fake), INVALID), (dict(S=1 << 30, Hq=8, Hk=8), UNSUPPORTED),
+    (dict(q_offsets=fake + 2), INVALID), (dict(k_lengths=fake + 1), INVALID), (dict(slope=fake, q_pos=fake, k_pos=fake + 2), INVALID),
 ])
 def test_attention_refuses_bad_arguments(lib, kw, code):
     h = heads(token=1 << 14, head=136)
