@@ -334,7 +334,16 @@ __global__ __launch_bounds__(64 * KEYW * SHARE, KEYW == 1 && DP * sizeof(T) > 12
     __shared__ __align__(16) typename M::E qs[BN * M::LD];
     __shared__ __align__(16) typename M::E gs[BN * M::LD];
     __shared__ __align__(16) float par[ROW_LINES][BN];
-    __shared__ __align__(16) u32x4 passed[SHARE > 1 ? KEYW * SHARE : 1][2][SHARE > 1 ? M::WEIGHT_VECTORS * 64 : 1];
+    constexpr bool FINE = KEYW == 1;      // few keys: factors as two bf16 each, as in the forward pass of few rows
+    __shared__ __align__(16) u32x4 passed[SHARE > 1 ? KEYW * SHARE : 1][2][SHARE > 1 ? (FINE ? M::FINE_VECTORS : M::WEIGHT_VECTORS) * 64 : 1];
+    auto factors = [](const f32x16& f) {
+        if constexpr (FINE) return M::fine(f);
+        else return M::weights(f);
+    };
+    auto fetched = [](const u32x4* from) {
+        if constexpr (FINE) return M::get_fine(from);
+        else return M::get(from);
+    };
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = (tid >> 6) % KEYW, share = (tid >> 6) / KEYW;
     const int head_k = blockIdx.x % A.Hk, Hq = A.Hk * A.group;
     const int64_t tile = blockIdx.x / A.Hk;
@@ -451,22 +460,22 @@ __global__ __launch_bounds__(64 * KEYW * SHARE, KEYW == 1 && DP * sizeof(T) > 12
             for (int m = 0; m < n; m += 32) {
                 f32x16 p, ds;
                 weigh(m, p, ds);
-                M::accumulate(dv, gs, m, M::weights(p), lane);
-                M::accumulate(dk, qs, m, M::weights(ds), lane);
+                M::accumulate(dv, gs, m, factors(p), lane);
+                M::accumulate(dk, qs, m, factors(ds), lane);
             }
         } else {
             if (busy) {
                 f32x16 p, ds;
                 weigh(32 * share, p, ds);
-                M::put(&passed[share * KEYW + wave][0][lane], M::weights(p));
-                M::put(&passed[share * KEYW + wave][1][lane], M::weights(ds));
+                M::put(&passed[share * KEYW + wave][0][lane], factors(p));
+                M::put(&passed[share * KEYW + wave][1][lane], factors(ds));
             }
             __syncthreads();
             if (busy) {
 #pragma unroll
                 for (int u = 0; u < SHARE; ++u) {
-                    M::accumulate(dv, gs + share * NT * 32, 32 * u, M::get(&passed[u * KEYW + wave][0][lane]), lane);
-                    M::accumulate(dk, qs + share * NT * 32, 32 * u, M::get(&passed[u * KEYW + wave][1][lane]), lane);
+                    M::accumulate(dv, gs + share * NT * 32, 32 * u, fetched(&passed[u * KEYW + wave][0][lane]), lane);
+                    M::accumulate(dk, qs + share * NT * 32, 32 * u, fetched(&passed[u * KEYW + wave][1][lane]), lane);
                 }
             }
         }
