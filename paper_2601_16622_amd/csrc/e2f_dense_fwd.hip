@@ -270,11 +270,11 @@ FwdPlan fwd_plan(const e2f_dense_args* a) {
     if (P.tiles == 0) return P;
     const int64_t blocks = P.tiles * a->Hk, keys = a->Nk / S;
     if (P.roww == 4) {
-        // two workgroups to a compute unit; a round over 10 000 keys with 64 (128) features takes 354 (524) us in bf16, 900 (1 500) in
-        // fp32.  Two parts instead of one: 10 000 atoms, 8 heads, 632 workgroups 708 -> 587 us; 4 000 atoms in fp32, 264 workgroups,
-        // 359 -> 367, and stays in one
-        const double per_key = a->dtype == E2F_BF16 ? 0.018 + 0.00027 * a->D : 0.03 + 0.00094 * a->D;
-        P.parts = best_parts(blocks, 512, keys * per_key, rows * a->Hk * (a->D * 8.0) / 4.5e6, keys / 256);
+        // two workgroups to a compute unit; a round over 10 000 keys with 64 (128) features takes 354 (524) us in bf16, 800 (1 500) in
+        // fp32.  Parts instead of one: 10 000 atoms, 8 heads, 632 workgroups 708 -> 569 us with two; 4 000 atoms in fp32, 264 workgroups,
+        // 309 -> 233 with three.  At most JOIN_FEW, beyond which joining many rows takes longer than their sums (9 000 atoms, 2.3 ms)
+        const double per_key = a->dtype == E2F_BF16 ? 0.018 + 0.00027 * a->D : 0.02 + 0.001 * a->D;
+        P.parts = best_parts(blocks, 512, keys * per_key, rows * a->Hk * (a->D * 8.0) / 4.5e6, keys / 256 < JOIN_FEW ? keys / 256 : JOIN_FEW);
     } else {
         // a few rows: their keys over 2048 waves, each with two tiles at least
         int64_t parts = 2048 / (blocks * P.keyw);
