@@ -611,21 +611,22 @@ void launch_dp(const DenseParams& A, const BwdPlan& P, hipStream_t st) {
     const dim3 stats((unsigned)(P.row_tiles * A.Hk), (unsigned)P.stat_parts), rows(stats.x, (unsigned)P.row_parts),
         keys((unsigned)(P.key_tiles * A.Hk), (unsigned)P.key_parts);
     const int64_t n = (int64_t)A.Nq * A.Hk * A.group;
-    // more than 64 features: two waves to a group of rows or keys; of keys also beyond 32 features in fp32 (48 features, 4 x 1 000 atoms: rows
-    // 215 us with two waves and 199 with one, keys 196 and 245)
+    // workgroups of many rows or keys with more than 64 features: two waves to a group of 32; of keys also beyond 32 features in fp32 (48
+    // features, 4 x 1 000 atoms: rows 215 us with two waves and 147 with one, keys 197 and 245).  Workgroups of one wave have the
+    // registers for all of it, and its LDS would leave a compute unit one workgroup
     constexpr int KD = DP > 64 ? 128 : DP, SHARE = DP > 64 ? 2 : 1, KEY_SHARE = DP * sizeof(T) > 128 ? 2 : 1;
     if (rows.x) {
         if (P.row_waves == 4) k_dense_bwd_stats<T, DP, 4><<<stats, 256, 0, st>>>(A);
         else k_dense_bwd_stats<T, DP, 1><<<stats, 64, 0, st>>>(A);
         if (P.stat_parts > 1) k_dense_bwd_join_stats<<<(unsigned)((n + SUM_THREADS - 1) / SUM_THREADS), SUM_THREADS, 0, st>>>(A, P.stat_parts);
         if (P.row_waves == 4) k_dense_bwd_rows<T, KD, 4, SHARE><<<rows, 256 * SHARE, 0, st>>>(A);
-        else k_dense_bwd_rows<T, KD, 1, SHARE><<<rows, 64 * SHARE, 0, st>>>(A);
+        else k_dense_bwd_rows<T, DP, 1, 1><<<rows, 64, 0, st>>>(A);
     }
     if (keys.x) {
         auto go = [&](auto cap, auto bias) {
             constexpr bool CAP = decltype(cap)::value, BIAS = decltype(bias)::value;
             if (P.key_waves == 4) k_dense_bwd_keys<T, KD, 4, KEY_SHARE, CAP, BIAS><<<keys, 256 * KEY_SHARE, 0, st>>>(A);
-            else k_dense_bwd_keys<T, KD, 1, KEY_SHARE, CAP, BIAS><<<keys, 64 * KEY_SHARE, 0, st>>>(A);
+            else k_dense_bwd_keys<T, DP, 1, 1, CAP, BIAS><<<keys, 64, 0, st>>>(A);
         };
         const std::true_type yes;
         const std::false_type no;

@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256) void k_dense_join_few(DenseParams A, int parts
     else *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
 }
 
-// For many parts of a few rows, a workgroup for a row; its waves share the parts, a lane forms a part's factor, then all lanes walk over the features of the wave's parts, whose loads do
+// For many parts of rows that do not fill the chip so, a workgroup for a row; its waves share the parts, a lane forms a part's factor, then all lanes walk over the features of the wave's parts, whose loads do
 // not wait for each other.
 constexpr int JOIN_WAVES = 16, JOIN_FEW = 8;
 template <typename T>
@@ -272,9 +272,10 @@ FwdPlan fwd_plan(const e2f_dense_args* a) {
     if (P.roww == 4) {
         // two workgroups to a compute unit; a round over 10 000 keys with 64 (128) features takes 354 (524) us in bf16, 800 (1 500) in
         // fp32.  Parts instead of one: 10 000 atoms, 8 heads, 632 workgroups 708 -> 569 us with two; 4 000 atoms in fp32, 264 workgroups,
-        // 309 -> 233 with three.  At most JOIN_FEW, beyond which joining many rows takes longer than their sums (9 000 atoms, 2.3 ms)
+        // 309 -> 233 with three; 100 queries over 60 000 keys on 2 key heads 291 us with eight parts,
+        // 79 with 64
         const double per_key = a->dtype == E2F_BF16 ? 0.018 + 0.00027 * a->D : 0.02 + 0.001 * a->D;
-        P.parts = best_parts(blocks, 512, keys * per_key, rows * a->Hk * (a->D * 8.0) / 4.5e6, keys / 256 < JOIN_FEW ? keys / 256 : JOIN_FEW);
+        P.parts = best_parts(blocks, 512, keys * per_key, rows * a->Hk * (a->D * 8.0) / 4.5e6, keys / 256);
     } else {
         // a few rows: their keys over 2048 waves, each with two tiles at least
         int64_t parts = 2048 / (blocks * P.keyw);
@@ -292,7 +293,7 @@ void launch_dp(const DenseParams& A, const FwdPlan& P, hipStream_t st) {
     else if (P.keyw == 4) k_dense_fwd<T, DP, 1, 4><<<grid, 256, 0, st>>>(A);
     else k_dense_fwd<T, DP, 1, 1><<<grid, 64, 0, st>>>(A);
     const int64_t rows = (int64_t)A.Nq * A.Hk * A.group;
-    if (P.parts > JOIN_FEW) k_dense_join<T><<<(unsigned)rows, 64 * JOIN_WAVES, 0, st>>>(A, P.parts);
+    if (P.parts > JOIN_FEW && rows * (A.D / 4) < 65536) k_dense_join<T><<<(unsigned)rows, 64 * JOIN_WAVES, 0, st>>>(A, P.parts);
     else if (P.parts > 1) k_dense_join_few<T><<<(unsigned)((rows * (A.D / 4) + 255) / 256), 256, 0, st>>>(A, P.parts);
 }
 

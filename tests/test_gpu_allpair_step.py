@@ -114,7 +114,7 @@ def test_two_streams_at_once():
         assert all(torch.equal(g[n], w[n]) for n in g)
 
 
-@pytest.mark.parametrize("nk,queries", [(5000, 1), (20000, 1), (3000, 5), (200, 1)])
+@pytest.mark.parametrize("nk,queries", [(5000, 1), (20000, 1), (3000, 5), (200, 1), (20000, 40)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_readout_equals_the_row_of_a_full_call(dtype, nk, queries):
     """A few queries over a system (keys split over waves and workgroups) against the same rows among many."""
