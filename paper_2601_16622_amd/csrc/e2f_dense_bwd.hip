@@ -4,8 +4,9 @@
 //   dslope_h = - sum ds d;  dr_i = - sum_{h,j} slope_h ds (r_i - r_j) / d,  dr_j the opposite
 // Nothing of a pair is stored: a kernel over rows forms the softmax statistics and delta, a second one dq, a kernel over keys
 // dk and dv.  Each sum is formed by the workgroup that owns its row or key, so no atomics are needed; where these are too few to
-// fill the chip the other side is cut into parts, whose sums are joined in their order.  delta comes from the binary32 products and weights (not from the rounded result of the forward pass):
-// the gradients of slope and places are binary32 and keep their precision.
+// fill the chip the other side is cut into parts, whose sums are joined in their order.  delta comes from the binary32 products
+// and weights (not from the rounded result of the forward pass): the gradients of slope and places are binary32 and keep their
+// precision.
 #include <type_traits>
 
 #include "e2f_dense_api.h"

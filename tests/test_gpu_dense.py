@@ -124,6 +124,10 @@ RAGGED = ([1, 0, 33, 128, 129, 64, 5], [1, 4, 31, 130, 0, 65, 257])
     (48, 6, 2, *RAGGED, 3.0, False), (64, 2, 2, [300], [300], 30.0, True), (64, 8, 2, [1, 1, 1], [700, 3, 64], 30.0, True),
     (80, 3, 3, [40, 41], [100, 99], 0.0, False), (96, 4, 2, [70], [129], 10.0, True), (104, 2, 1, [65], [66], 0.0, True),
     (128, 4, 1, [33, 90], [200, 31], 50.0, True), (128, 16, 1, [9], [500], 0.0, False),
+    # few rows and keys, few rows over many keys, with many features; a group of heads larger than a tile
+    (128, 2, 2, [20, 30], [40, 10], 20.0, True), (96, 2, 1, [10, 0, 25], [30, 7, 64], 0.0, True), (72, 3, 3, [33, 64], [12, 33], 6.0, False),
+    (128, 8, 2, [1, 2], [700, 300], 30.0, True), (88, 4, 4, [2], [1100], 0.0, False), (32, 4, 2, [3, 1], [900, 260], 10.0, True),
+    (16, 200, 1, [3, 1], [40, 150], 10.0, True),
 ])
 def test_against_64_bits(dtype, D, Hq, Hk, nq, nk, cap, biased):
     check(make(dtype, D, Hq, Hk, nq, nk, biased, D + Hq), cap)
