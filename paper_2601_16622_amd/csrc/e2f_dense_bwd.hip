@@ -192,16 +192,15 @@ __global__ __launch_bounds__(SUM_THREADS) void k_dense_bwd_join_stats(DenseParam
     if (A.score.biased) A.usual[row] = usual * inv;
 }
 
-// dq and a row's shares of the gradients of slope and place, from the statistics.  In bf16 the factors of the sum over k are two bf16 each: a
-// row's factors sum up to nothing, and what the rounding of one leaves of dq would come close to twice its own rounding's share.  SHARE waves to a group of rows pass each other the
-// weights and keep the sums of DP / SHARE features each, as in the kernel over keys.
+// dq and a row's shares of the gradients of slope and place, from the statistics.  SHARE waves to a group of rows pass each other the weights and
+// keep the sums of DP / SHARE features each, as in the kernel over keys.
 template <typename T, int DP, int ROWW, int SHARE>
 __global__ __launch_bounds__(64 * ROWW * SHARE, ROWW == 1 && DP * sizeof(T) > 128 ? 1 : 2) void k_dense_bwd_rows(DenseParams A) {
     using R = RowWalk<T, DP, ROWW, SHARE>;
     using M = typename R::M;
     constexpr int BN = R::BN, NT = DP / SHARE / 32;
     __shared__ __align__(16) typename R::Tile tile;
-    __shared__ __align__(16) u32x4 passed[SHARE > 1 ? ROWW * SHARE : 1][SHARE > 1 ? M::FINE_VECTORS * 64 : 1];
+    __shared__ __align__(16) u32x4 passed[SHARE > 1 ? ROWW * SHARE : 1][SHARE > 1 ? M::WEIGHT_VECTORS * 64 : 1];
     R w(A);
     const int Hq = A.Hk * A.group;
     float* slopes = A.slope_part ? A.slope_part + ((int64_t)blockIdx.y * (gridDim.x / A.Hk) + blockIdx.x / A.Hk) * Hq + w.head_k * A.group : nullptr;
@@ -256,7 +255,7 @@ __global__ __launch_bounds__(64 * ROWW * SHARE, ROWW == 1 && DP * sizeof(T) > 12
 #pragma unroll
             for (int i = 0; i < 16; ++i) p[i] *= slack[i];
         }
-        return M::fine(p);
+        return M::weights(p);
     };
     if constexpr (SHARE == 1) {
         w.walk(A, tile, [&](int m, int n) { M::accumulate(acc, tile.k, m, weigh(m, n), w.lane); });
@@ -267,7 +266,7 @@ __global__ __launch_bounds__(64 * ROWW * SHARE, ROWW == 1 && DP * sizeof(T) > 12
             if (w.busy) {
 #pragma unroll
                 for (int u = 0; u < SHARE; ++u)
-                    M::accumulate(acc, tile.k + w.share * NT * 32, 32 * u, M::get_fine(&passed[u * ROWW + w.group][w.lane]), w.lane);
+                    M::accumulate(acc, tile.k + w.share * NT * 32, 32 * u, M::get(&passed[u * ROWW + w.group][w.lane]), w.lane);
             }
         });
     }
@@ -335,16 +334,7 @@ __global__ __launch_bounds__(64 * KEYW * SHARE, KEYW == 1 && DP * sizeof(T) > 12
     __shared__ __align__(16) typename M::E qs[BN * M::LD];
     __shared__ __align__(16) typename M::E gs[BN * M::LD];
     __shared__ __align__(16) float par[ROW_LINES][BN];
-    constexpr bool FINE = KEYW == 1;      // few keys: factors as two bf16 each, as in the forward pass of few rows
-    __shared__ __align__(16) u32x4 passed[SHARE > 1 ? KEYW * SHARE : 1][2][SHARE > 1 ? (FINE ? M::FINE_VECTORS : M::WEIGHT_VECTORS) * 64 : 1];
-    auto factors = [](const f32x16& f) {
-        if constexpr (FINE) return M::fine(f);
-        else return M::weights(f);
-    };
-    auto fetched = [](const u32x4* from) {
-        if constexpr (FINE) return M::get_fine(from);
-        else return M::get(from);
-    };
+    __shared__ __align__(16) u32x4 passed[SHARE > 1 ? KEYW * SHARE : 1][2][SHARE > 1 ? M::WEIGHT_VECTORS * 64 : 1];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = (tid >> 6) % KEYW, share = (tid >> 6) / KEYW;
     const int head_k = blockIdx.x % A.Hk, Hq = A.Hk * A.group;
     const int64_t tile = blockIdx.x / A.Hk;
@@ -461,22 +451,22 @@ __global__ __launch_bounds__(64 * KEYW * SHARE, KEYW == 1 && DP * sizeof(T) > 12
             for (int m = 0; m < n; m += 32) {
                 f32x16 p, ds;
                 weigh(m, p, ds);
-                M::accumulate(dv, gs, m, factors(p), lane);
-                M::accumulate(dk, qs, m, factors(ds), lane);
+                M::accumulate(dv, gs, m, M::weights(p), lane);
+                M::accumulate(dk, qs, m, M::weights(ds), lane);
             }
         } else {
             if (busy) {
                 f32x16 p, ds;
                 weigh(32 * share, p, ds);
-                M::put(&passed[share * KEYW + wave][0][lane], factors(p));
-                M::put(&passed[share * KEYW + wave][1][lane], factors(ds));
+                M::put(&passed[share * KEYW + wave][0][lane], M::weights(p));
+                M::put(&passed[share * KEYW + wave][1][lane], M::weights(ds));
             }
             __syncthreads();
             if (busy) {
 #pragma unroll
                 for (int u = 0; u < SHARE; ++u) {
-                    M::accumulate(dv, gs + share * NT * 32, 32 * u, fetched(&passed[u * KEYW + wave][0][lane]), lane);
-                    M::accumulate(dk, qs + share * NT * 32, 32 * u, fetched(&passed[u * KEYW + wave][1][lane]), lane);
+                    M::accumulate(dv, gs + share * NT * 32, 32 * u, M::get(&passed[u * KEYW + wave][0][lane]), lane);
+                    M::accumulate(dk, qs + share * NT * 32, 32 * u, M::get(&passed[u * KEYW + wave][1][lane]), lane);
                 }
             }
         }

@@ -98,10 +98,7 @@ __global__ __launch_bounds__(64 * ROWW * KEYW, ROWW == 1 && DP * sizeof(T) > 128
                 add += p[i];
             }
             sum += add;
-            // one wave's rows are few, and their results: with the weights as two bf16 the error of these is the rounding of the result
-            // alone, where the other roundings would add half of it again (vector work does not bound these calls)
-            if constexpr (ROWW == 1) M::accumulate(acc, tile.v, m, M::fine(p), lane);
-            else M::accumulate(acc, tile.v, m, M::weights(p), lane);
+            M::accumulate(acc, tile.v, m, M::weights(p), lane);
         }
     }
     sum += other_half(sum);

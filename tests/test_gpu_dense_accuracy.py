@@ -1,0 +1,74 @@
+"""Attention among all atoms of a segment: how far each value of a result may be from 64 bits, where the tests by norms see little.
+
+Tolerance of a value, u = 2^-24 (fp32).  It is the sum of terms t_i, each a product with relative error d_i, rounded once at the end by
+h (bf16 2^-8, fp32 u): |got - want| <= h |want| + sum |t_i| d_i.  In d:
+  - a product of D features is off by (D + 8) u of the sum of its terms' sizes (raw), by 8 u more where a value is three bf16
+    and the three smallest of the nine partial products are left out (each below 2^-22 of the product);
+  - a score s that is off by that much of raw and, with a cap, by 2^-22 of the cap (the exponential form in bf16, up to a cap of 128) shifts a
+    weight by twice that (the weight itself and its row's sum), and by 16 u for exponentials, distances and divisions;
+  - weights and factors that enter a product are off by 2^-15 in bf16 (two bf16, the first cut, the second rounded: 2^-7 * 2^-8) and
+    by 8 u in fp32, and sums over n terms by n u."""
+import math
+
+import pytest
+import torch
+
+import allpair_reference as R
+from paper_2601_16622_amd import binding as B
+from test_gpu_dense import DT, U, call, make, reference
+
+pytestmark = pytest.mark.gpu
+
+
+def limits(x, cap=0.0, scale=None):
+    """Per value of out, q, k and v: the largest distance from 64 bits without the rounding of the result."""
+    D, Hq, Hk = x["q"].shape[2], x["q"].shape[1], x["k"].shape[1]
+    scale = D ** -0.5 if scale is None else scale
+    bf16 = x["q"].dtype == torch.bfloat16
+    q, k, v, go = (x[n].double().cpu() for n in ("q", "k", "v", "go"))
+    at = [x[n].double().cpu() if x.get(n) is not None else None for n in ("q_pos", "k_pos", "slope")]
+    got = dict(out=torch.zeros_like(q), q=torch.zeros_like(q), k=torch.zeros_like(k), v=torch.zeros_like(v))
+    lists = {n: (x[n].tolist() if x.get(n) is not None else None) for n in ("q_offsets", "k_offsets", "q_lengths", "k_lengths")}
+    for (a, n), (b, m) in zip(R.ranges(lists["q_offsets"], lists["q_lengths"], q.shape[0]), R.ranges(lists["k_offsets"], lists["k_lengths"], k.shape[0])):
+        if n == 0 or m == 0:
+            continue
+        for h in range(Hq):
+            g = h * Hk // Hq
+            Q, K, V, G = q[a:a + n, h], k[b:b + m, g], v[b:b + m, g], go[a:a + n, h]
+            s = R.dense_scores(Q, K, scale, cap, *((at[0][a:a + n], at[1][b:b + m], at[2][h]) if at[2] is not None else (None,) * 3))
+            raw = abs(scale) * (Q.abs() @ K.abs().T)
+            slack = (1 - torch.tanh(scale * (Q @ K.T) / cap).square()) if cap else 1.0
+            near = (D + 16) * U * raw * slack + 16 * U * s.abs().amax() + (2.0 ** -22 * min(cap, 128.0) if bf16 else 4 * U * cap)
+            d = 2 * near.amax() + 16 * U
+            last = (2.0 ** -15 if bf16 else 8 * U) + max(n * Hq // Hk, m) * U
+            p, A = torch.softmax(s, -1), G.abs() @ V.abs().T
+            got["out"][a:a + n, h] = (d + last) * (p @ V.abs())
+            got["v"][b:b + m, g] += (d + last) * (p.T @ G.abs())
+            # ds = p (dp - delta): p and delta off by d and the sums over the keys, dp and delta by the products over the features
+            size = p * (A + (p * A).sum(-1, keepdim=True))
+            # the slack: 1 - tanh^2 at an argument that is off by its product's error, relative to it twice that, and 16 u of its own
+            dx = size * slack * (2 * d + last + (D + 16 + m) * U + (2 * (D + 16) * U * raw / cap if cap else 0.0) + 16 * U)
+            got["q"][a:a + n, h] = abs(scale) * (dx @ K.abs())
+            got["k"][b:b + m, g] += abs(scale) * (dx.T @ Q.abs())
+    return got
+
+
+def check_values(x, cap=0.0, scale=None, rows=slice(None)):
+    want, covered, k_covered, _, _ = reference(x, cap, scale)
+    most, got = limits(x, cap, scale), call(x, cap, scale)
+    h = 2.0 ** -8 if x["q"].dtype == torch.bfloat16 else U
+    for name, e in most.items():
+        w, g = want[name], got[name].double().cpu()
+        ok = (g - w).abs() <= h * (w.abs() + e) + e
+        ok = ok[k_covered if name in "kv" else covered][rows if name in ("out", "q") else slice(None)]
+        far = ((g - w).abs() / (h * (w.abs() + e) + e))[k_covered if name in "kv" else covered]
+        assert bool(ok.all()), (name, int((~ok).sum()), float(far.max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,Hq,Hk,nq,nk,cap", [
+    (64, 2, 2, [300], [300], 20.0), (32, 4, 1, [200, 0, 3], [170, 9, 200], 0.0), (128, 4, 2, [150], [210], 30.0), (80, 2, 1, [100, 30], [131, 20], 50.0),
+    (64, 2, 2, [20], [30], 20.0), (64, 4, 2, [1], [900], 20.0),
+])
+def test_every_value(dtype, D, Hq, Hk, nq, nk, cap):
+    check_values(make(dtype, D, Hq, Hk, nq, nk, True, D + Hq + len(nq)), cap)
