@@ -417,7 +417,8 @@ e2f_status e2f_qk_norm_rotate_backward(const e2f_qk_args *a, const e2f_heads *q,
  * rows of out and of the gradients that no segment's length covers are left as they were.  No result may overlap an operand or
  * another result.  A row's result is the same bits whatever the rows beside it hold.
  * Scores, softmax statistics and sums are binary32; with bf16 features the weights and factors that meet the matrix cores are the sum of two
- * bf16 each, off by 2^-15 at most.  The gradients of slope and places take no such rounding.
+ * bf16 each, off by 2^-15 at most, and the forward pass's scores under a cap of up to 128 are off by 2^-22 of the cap at most.  The gradients of
+ * slope and places take no such rounding.
  */
 typedef struct {
     int32_t dtype;          /* e2f_dtype of q, k, v, out and their gradients */

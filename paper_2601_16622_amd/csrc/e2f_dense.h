@@ -25,6 +25,7 @@ struct DenseScore {
     float out, inv_out;  // cap log2(e) and its reciprocal
     float c[8];          // odd polynomial of out * tanh
     int32_t capped, biased;
+    int32_t coarse;      // the tanh by exponential and reciprocal serves results in bf16 (or there is no cap)
 };
 
 struct DenseParams {
@@ -541,7 +542,9 @@ __device__ __forceinline__ void cap_scores(f32x16& p, f32x16& slack, const Dense
 }
 
 // The same with tanh x = 1 - 2 / (1 + e^2x) everywhere: 7 issue slots an element (the exponential and the reciprocal take two each)
-// where the polynomial and its vote take 11.  Its absolute error, 2^-23 of the cap, is for results in bf16 alone.
+// where the polynomial and its vote take 11.  Its absolute error, 2^-23 of the cap whatever the score, shifts a weight by 2^-15 at a cap of
+// 128, as the weights' own rounding for the matrix cores does: it is for results in bf16 and caps up to that (at 2^20 it is 10 % of a weight).
+constexpr float COARSE_CAP = 128.0f;
 __device__ __forceinline__ void cap_scores_coarse(f32x16& p, const DenseScore& A, float base) {
     if (!A.capped) {
         plain_scores(p, A, base);

@@ -77,7 +77,7 @@ __global__ __launch_bounds__(64 * ROWW * KEYW, ROWW == 1 && DP * sizeof(T) > 128
         const int n = min(BN, end - t);
         for (int m = 0; m < n; m += 32) {
             f32x16 p = M::dot(tile.k, m, qf, lane);
-            if constexpr (sizeof(T) == 2) cap_scores_coarse(p, A.score, reference_base(top));
+            if (sizeof(T) == 2 && A.score.coarse) cap_scores_coarse(p, A.score, reference_base(top));
             else cap_scores<false>(p, p, A.score, reference_base(top));
             if (A.score.biased) bias_scores<BN>(p, x, y, z, slope, tile.place, m + 4 * half);
             if (n - m < 32) {
@@ -369,6 +369,7 @@ void dense_fill(DenseParams& A, const e2f_dense_args* a, const e2f_heads* q, con
     DenseScore& s = A.score;
     s.capped = a->cap > 0.0f;
     s.biased = a->slope != nullptr;
+    s.coarse = a->cap <= COARSE_CAP;
     s.in = s.capped ? a->scale / a->cap : (float)((double)a->scale * 1.4426950408889634);
     const double out = (double)a->cap * 1.4426950408889634;
     s.out = (float)out;

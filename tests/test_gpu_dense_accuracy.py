@@ -46,8 +46,9 @@ def limits(x, cap=0.0, scale=None):
             got["v"][b:b + m, g] += (d + last) * (p.T @ G.abs())
             # ds = p (dp - delta): p and delta off by d and the sums over the keys, dp and delta by the products over the features
             size = p * (A + (p * A).sum(-1, keepdim=True))
-            # the slack: 1 - tanh^2 at an argument that is off by its product's error, relative to it twice that, and 16 u of its own
-            dx = size * slack * (2 * d + last + (D + 16 + m) * U + (2 * (D + 16) * U * raw / cap if cap else 0.0) + 16 * U)
+            # the slack: 1 - tanh^2 at an argument that is off by its product's error, relative to it twice that, and 16 u of its own; and in the
+            # reference a difference from 1 in 64 bits, off by 2^-52
+            dx = size * (slack * (2 * d + last + (D + 16 + m) * U + (2 * (D + 16) * U * raw / cap if cap else 0.0) + 16 * U) + 2.0 ** -52)
             got["q"][a:a + n, h] = abs(scale) * (dx @ K.abs())
             got["k"][b:b + m, g] += abs(scale) * (dx.T @ Q.abs())
     return got
@@ -72,3 +73,11 @@ def check_values(x, cap=0.0, scale=None, rows=slice(None)):
 ])
 def test_every_value(dtype, D, Hq, Hk, nq, nk, cap):
     check_values(make(dtype, D, Hq, Hk, nq, nk, True, D + Hq + len(nq)), cap)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cap", [2.0 ** -20, 0.5, 127.0, 129.0, 1e3, 2.0 ** 14, 1e5, 2.0 ** 20])
+def test_caps_over_the_whole_range(dtype, cap):
+    """Scores of a usual size under every cap that is accepted: many rows, few rows, and few rows over many keys."""
+    for nq, nk in (([200], [260]), ([20], [40]), ([1], [600])):
+        check_values(make(dtype, 64, 2, 1, nq, nk, True, 31), cap)
