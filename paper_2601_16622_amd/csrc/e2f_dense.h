@@ -486,7 +486,7 @@ __device__ __forceinline__ void tile_sync() {
 }
 
 // p (products q . k) -> scores minus base; SLACK: slack = 1 - tanh^2.  The tanh of an argument x up to 1 is an odd polynomial (relative
-// error 8e-8; scores are rarely near their cap), beyond that 1 - 2 / (1 + e^2x), whose absolute error of 1e-7 is then a relative one.
+// error 8e-8; scores are rarely near their cap), beyond that 1 - 2 / (1 + e^2|x|) with the sign of x, whose absolute error of 1e-7 is then a relative one.
 // Which form an element gets goes by the element alone, so that a row's result does not depend on the rows beside it; the
 // vote only leaves the second form out where no element of the wave needs it.
 // The largest argument's size of a lane; beyond 1 in any lane of the wave (`__any`), FAR is asked for.
@@ -515,10 +515,11 @@ __device__ __forceinline__ void cap_values(f32x16& p, f32x16& slack, const Dense
             p[i] = x * t - base;
         }
         if (FAR) {
-            const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f * LOG2E)));
+            // from |x|: r is at most 0.12 then, and 1 - r keeps its precision at either sign
+            const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(fabsf(x) * (2.0f * LOG2E)));
             if (fabsf(x) > 1.0f) {
                 if (SLACK) slack[i] = 4.0f * r * (1.0f - r);       // 1 - (1 - 2 r)^2
-                p[i] = (1.0f - 2.0f * r) * A.out - base;
+                p[i] = copysignf((1.0f - 2.0f * r) * A.out, x) - base;
             }
         }
     }

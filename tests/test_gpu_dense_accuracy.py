@@ -81,3 +81,15 @@ def test_caps_over_the_whole_range(dtype, cap):
     """Scores of a usual size under every cap that is accepted: many rows, few rows, and few rows over many keys."""
     for nq, nk in (([200], [260]), ([20], [40]), ([1], [600])):
         check_values(make(dtype, 64, 2, 1, nq, nk, True, 31), cap)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("level", [1.5, 4.0, 6.0, 7.5, 9.0, 12.0])
+def test_scores_at_the_cap(dtype, sign, level):
+    """Queries along or against all keys, every score near +-cap: 1 - tanh^2 is small there and grad_q and grad_k are products with it."""
+    x = make(dtype, 32, 2, 1, [70], [90], True, 32)
+    cap, base = 10.0, torch.randn(32, generator=torch.Generator().manual_seed(1)).cuda()
+    x["k"] = (base + 0.05 * x["k"].float()).to(DT[dtype])
+    x["q"] = (sign * level * cap * 32 ** 0.5 * base / base.square().sum() + 0.05 * x["q"].float()).to(DT[dtype])
+    check_values(x, cap)
