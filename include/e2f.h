@@ -424,7 +424,7 @@ typedef struct {
     int32_t dtype;          /* e2f_dtype of q, k, v, out and their gradients */
     int32_t Hq, Hk;         /* query and key heads, Hq a multiple of Hk, 1..1024 */
     int32_t D;              /* features of a head, a multiple of 8, 8..128 */
-    int32_t Nq, Nk, S;      /* query tokens, key tokens, segments */
+    int32_t Nq, Nk, S;      /* query tokens, key tokens, segments; Nq Hq/Hk and Nk up to 2^31 - 1025 */
     float scale;            /* finite */
     float cap;              /* 2^-20 .. 2^20, or 0 for none */
     const int32_t *q_offsets, *k_offsets, *q_lengths, *k_lengths;

@@ -323,9 +323,10 @@ e2f_status dense_check_sizes(const e2f_dense_args* a) {
     if (a->D % 8 || a->D > 128 || a->Hq > 1024) return E2F_ERR_UNSUPPORTED;
     // far from where the constants of the tanh leave binary32
     if (a->cap > 0.0f && (a->cap < 0x1p-20f || a->cap > 0x1p20f)) return E2F_ERR_UNSUPPORTED;
-    // the grid of either direction and the stacked rows of a segment are 31-bit numbers
+    // the grid of either direction and the stacked rows of a segment are 31-bit numbers, and so are the counters that walk over rows and
+    // keys by tiles, a step beyond their end
     const int64_t most = INT32_MAX / a->Hk;
-    if ((int64_t)a->Nq * (a->Hq / a->Hk) > INT32_MAX - 1024) return E2F_ERR_UNSUPPORTED;
+    if ((int64_t)a->Nq * (a->Hq / a->Hk) > INT32_MAX - 1024 || a->Nk > INT32_MAX - 1024) return E2F_ERR_UNSUPPORTED;
     if (dense_tiles(a->Nq, a->Hq / a->Hk, a->S, 32) > most || dense_tiles(a->Nk, 1, a->S, 32) > most)
         return E2F_ERR_UNSUPPORTED;
     return E2F_OK;
