@@ -412,10 +412,12 @@ e2f_status e2f_qk_norm_rotate_backward(const e2f_qk_args *a, const e2f_heads *q,
  *                 tokens there are): segment s has the queries [q_offsets[s], q_offsets[s+1]), the keys likewise
  *   q_lengths, k_lengths  device int32 [S] or NULL: only the first tokens of each segment count (a padded batch); values
  *                 are cut to 0 .. the segment's size
- *   q_pos, k_pos, slope   device float [Nq][3], [Nk][3], [Hq]; all three or none
+ *   q_pos, k_pos, slope   device float [Nq][3], [Nk][3], [Hq]; all three or none.  A coordinate beyond 5e18 in size, infinity too, counts as 5e18
  * Keys outside their segment's length and queries outside any segment's are not read.  A query without keys gets a zero row;
  * rows of out and of the gradients that no segment's length covers are left as they were.  No result may overlap an operand or
  * another result.  A row's result is the same bits whatever the rows beside it hold.
+ * A score s is off by 2^-22 of its size or so, and a weight with it: a query that is 2^20 / slope or farther from its nearest key has no
+ * meaningful weights, and what it brings to gradients may be NaN.
  * Scores, softmax statistics and sums are binary32; with bf16 features the weights and factors that meet the matrix cores are the sum of two
  * bf16 each, off by 2^-15 at most, and the forward pass's scores under a cap of up to 128 are off by 2^-22 of the cap at most.  The gradients of
  * slope and places take no such rounding.
@@ -443,7 +445,8 @@ e2f_status e2f_dense_attn_forward(const e2f_dense_args *a, const e2f_heads *q, c
  *   grad_q, grad_k, grad_v   rows of the feature type; gradients of a key head are summed over the query heads that share it
  *   grad_slope               device float [Hq], fully overwritten, or NULL
  *   grad_q_pos, grad_k_pos   device float [Nq][3], [Nk][3] or NULL: what q_pos and k_pos get as the queries' and as the keys'
- *                 places (add the two where they are the same atoms).  The distance of an atom to itself has gradient 0.
+ *                 places (add the two where they are the same atoms).  The distance of an atom to itself has gradient 0,
+ *                 towards which that of distances below 1e-18 falls.
  * The last three need slope (E2F_ERR_INVALID_ARG).
  */
 size_t e2f_dense_attn_backward_workspace_bytes(const e2f_dense_args *a);

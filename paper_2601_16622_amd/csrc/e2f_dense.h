@@ -453,6 +453,11 @@ struct Transfer {
     }
 };
 
+// A coordinate as it counts: within 5e18, so that the squares of a distance, (2 * 5e18)^2 three times, stay below 3.4e38.  Otherwise a key far away
+// (a place that says "not there") would have an infinite distance, which its weight of 0, or a slope of 0, turns into a NaN.  NaN stays NaN.
+constexpr float MOST_PLACE = 5e18f;
+__device__ __forceinline__ float place_of(float x) { return fabsf(x) > MOST_PLACE ? copysignf(MOST_PLACE, x) : x; }
+
 // The places of BN tokens likewise, into three lines of BN.
 template <int BN, int THREADS>
 struct PlaceTransfer {
@@ -469,7 +474,7 @@ struct PlaceTransfer {
 #pragma unroll
         for (int j = 0; j < EACH; ++j) {
             const int i = tid + j * THREADS;
-            if (i < 3 * BN) place[i % 3 * BN + i / 3] = x[j];
+            if (i < 3 * BN) place[i % 3 * BN + i / 3] = place_of(x[j]);
         }
     }
 };

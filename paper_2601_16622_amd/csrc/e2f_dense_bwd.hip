@@ -69,9 +69,9 @@ struct RowWalk {
         M::load(gf, A.go.row(query, head), A.D, valid, half);
         x = y = z = slope = 0;
         if (A.score.biased) {
-            x = A.q_pos[(int64_t)query * 3];
-            y = A.q_pos[(int64_t)query * 3 + 1];
-            z = A.q_pos[(int64_t)query * 3 + 2];
+            x = place_of(A.q_pos[(int64_t)query * 3]);
+            y = place_of(A.q_pos[(int64_t)query * 3 + 1]);
+            z = place_of(A.q_pos[(int64_t)query * 3 + 2]);
             slope = A.slope[head];
         }
     }
@@ -351,9 +351,9 @@ __global__ __launch_bounds__(64 * KEYW * SHARE, KEYW == 1 && DP * sizeof(T) > 12
     M::load(vf, A.v.row(key, head_k), A.D, valid, half);
     float x = 0, y = 0, z = 0;
     if (BIAS) {
-        x = A.k_pos[(int64_t)key * 3];
-        y = A.k_pos[(int64_t)key * 3 + 1];
-        z = A.k_pos[(int64_t)key * 3 + 2];
+        x = place_of(A.k_pos[(int64_t)key * 3]);
+        y = place_of(A.k_pos[(int64_t)key * 3 + 1]);
+        z = place_of(A.k_pos[(int64_t)key * 3 + 2]);
     }
     // this workgroup's part of the rows
     const int row_tiles = (rows + BN - 1) / BN, each = (row_tiles + (int)gridDim.y - 1) / (int)gridDim.y;
@@ -435,9 +435,9 @@ __global__ __launch_bounds__(64 * KEYW * SHARE, KEYW == 1 && DP * sizeof(T) > 12
         tq.store(tid, qs);
         tg.store(tid, gs);
         if (tid < BN) {
-            par[ROW_X][tid] = rx;
-            par[ROW_Y][tid] = ry;
-            par[ROW_Z][tid] = rz;
+            par[ROW_X][tid] = place_of(rx);
+            par[ROW_Y][tid] = place_of(ry);
+            par[ROW_Z][tid] = place_of(rz);
             par[ROW_SLOPE][tid] = rs;
             par[ROW_LSE][tid] = st.w;
             par[ROW_DELTA][tid] = st.z;

@@ -47,9 +47,9 @@ __global__ __launch_bounds__(64 * ROWW * KEYW, ROWW == 1 && DP * sizeof(T) > 128
     M::load(qf, A.q.row(query, head), A.D, valid, half);
     float x = 0, y = 0, z = 0, slope = 0;
     if (A.score.biased) {
-        x = A.q_pos[(int64_t)query * 3];
-        y = A.q_pos[(int64_t)query * 3 + 1];
-        z = A.q_pos[(int64_t)query * 3 + 2];
+        x = place_of(A.q_pos[(int64_t)query * 3]);
+        y = place_of(A.q_pos[(int64_t)query * 3 + 1]);
+        z = place_of(A.q_pos[(int64_t)query * 3 + 2]);
         slope = A.slope[head] * LOG2E;
     }
     f32x16 acc[DP / 32] = {};

@@ -93,3 +93,38 @@ def test_scores_at_the_cap(dtype, sign, level):
     x["k"] = (base + 0.05 * x["k"].float()).to(DT[dtype])
     x["q"] = (sign * level * cap * 32 ** 0.5 * base / base.square().sum() + 0.05 * x["q"].float()).to(DT[dtype])
     check_values(x, cap)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq,nk", [(80, 100), (5, 20), (1, 700), (300, 700)])
+@pytest.mark.parametrize("far", [1e19, 3e38, float("inf"), -float("inf")])
+def test_keys_far_away_are_as_keys_that_are_not_there(dtype, nq, nk, far):
+    """With a slope of 0.3 a key beyond 1e19 has weight 0: bit for bit as behind its segment's length.  Without one its weight is that of its product."""
+    x = make(dtype, 32, 2, 1, [nq], [nk], True, 33)
+    x["slope"] = torch.full_like(x["slope"], 0.3)
+    gone = dict(x, k_lengths=torch.tensor([nk - 3], dtype=torch.int32, device="cuda"))
+    want = call(gone, 20.0, fill=0.0)
+    y = dict(x, k_pos=x["k_pos"].clone())
+    y["k_pos"][nk - 3:] = far
+    y["k_pos"][nk - 1, 1:] = 1.0
+    got = call(y, 20.0)
+    for n in want:
+        assert torch.equal(got[n], want[n]), n
+    y["slope"] = x["slope"] * torch.tensor([0.0, 1.0], device="cuda")
+    got, plain = call(y, 20.0), call(dict(x, q_pos=None, k_pos=None, slope=None), 20.0)
+    assert torch.equal(got["out"][:, 0], plain["out"][:, 0]) and torch.equal(got["out"][:, 1], want["out"][:, 1])
+    assert all(bool(torch.isfinite(t).all()) for n, t in got.items())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_query_far_away_reaches_no_other_row(dtype):
+    """Its own scores of 1e18 have lost what tells keys apart; rows beside it have not."""
+    x = make(dtype, 32, 2, 2, [80], [100], True, 34)
+    want = call(x, 20.0)
+    x["q_pos"][11] = torch.tensor([1e30, -float("inf"), 2.0], device="cuda")
+    got = call(x, 20.0)
+    for n in ("out", "q", "q_pos"):
+        assert torch.equal(got[n][:11], want[n][:11]) and torch.equal(got[n][12:], want[n][12:])
+    x["q_pos"][11, 0] = float("nan")
+    got = call(x, 20.0, backward=False)["out"]
+    assert bool(torch.isnan(got[11]).all()) and torch.equal(got[12:], want["out"][12:])
