@@ -458,8 +458,8 @@ e2f_status e2f_dense_attn_backward(const e2f_dense_args *a, const e2f_heads *q, 
 /*
  * Global norm of a training step's gradients (those of e2f_attn_backward's weights, for instance) and clipping by it:
  *   norm = (sum over all elements of all tensors of g^2)^(1/2),  out = g * min(1, max_norm / (norm + 1e-6))
- * Squares and sums are binary64, so no finite gradient overflows.  If norm is not finite, out = g: the caller sees it in
- * *norm and skips the step.
+ * Squares and sums are binary64, so no finite gradient overflows: gradients are clipped by a norm beyond binary32 too, which *norm then shows as
+ * infinity.  If norm is not finite, out = g: the caller sees it in *norm and skips the step.
  *   n                 tensors, >= 0
  *   grads, out        host arrays [n] of device pointers, contiguous tensors; out[i] may be grads[i], any other overlap is
  *                     not allowed.  Tensors may start at any element.

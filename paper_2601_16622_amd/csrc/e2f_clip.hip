@@ -6,6 +6,8 @@
 // sum all of these (a few thousand, out of the L2) in the same order, which saves the launch and the wait of a
 // reduction of its own and gives every workgroup the same factor.  Tensors travel in the kernel's arguments, TENSORS of
 // them a launch, so that a captured graph needs no table in device memory.
+#include <float.h>
+
 #include "e2f_block.h"
 
 namespace {
@@ -98,20 +100,21 @@ __global__ __launch_bounds__(THREADS) void k_clip_squares(Batch B, double* parti
     if (threadIdx.x == 0) partial[b] = sum;
 }
 
-template <typename T>
-__device__ __forceinline__ void scaled(const T* p, T* q, int64_t n, float factor) {
+// F: float, or double where the factor is below binary32's normal numbers and would lose its last bits there.
+template <typename T, typename F>
+__device__ __forceinline__ void scaled(const T* p, T* q, int64_t n, F factor) {
     constexpr int V = Vec<T>::V;
     const int64_t whole = n / V * V;
     vectors(p, whole, [&](int64_t i, u32x4 x) {
         float f[V];
         Vec<T>::unpack(x, f);
 #pragma unroll
-        for (int u = 0; u < V; ++u) f[u] *= factor;
+        for (int u = 0; u < V; ++u) f[u] = (float)(f[u] * factor);
         *reinterpret_cast<Loose<T>*>(q + i) = Vec<T>::pack(f);
     });
     for (int64_t i = whole + threadIdx.x; i < n; i += THREADS) {
-        if constexpr (sizeof(T) == 4) q[i] = p[i] * factor;
-        else q[i] = (uint16_t)pack_bf16(__uint_as_float((uint32_t)p[i] << 16) * factor, 0.0f);
+        if constexpr (sizeof(T) == 4) q[i] = (float)(p[i] * factor);
+        else q[i] = (uint16_t)pack_bf16((float)(__uint_as_float((uint32_t)p[i] << 16) * factor), 0.0f);
     }
 }
 
@@ -139,15 +142,13 @@ __global__ __launch_bounds__(THREADS) void k_clip_scale(Batch B, const double* p
     const int t = tensor_of(B, b), first = B.first[t];
     const int64_t at = (int64_t)(b - (first & 0x7FFFFFFF)) * B.chunk, n = min(B.chunk, B.count[t] - at);
     const bool clip = ratio < 1.0 && root < (double)INFINITY;   // false for a NaN too
-    if (first < 0) {
-        const uint16_t* p = static_cast<const uint16_t*>(B.in[t]) + at;
-        uint16_t* q = static_cast<uint16_t*>(B.out[t]) + at;
-        if (clip) scaled(p, q, n, (float)ratio); else copied(p, q, n);
-    } else {
-        const float* p = static_cast<const float*>(B.in[t]) + at;
-        float* q = static_cast<float*>(B.out[t]) + at;
-        if (clip) scaled(p, q, n, (float)ratio); else copied(p, q, n);
-    }
+    auto chunk = [&](const auto* p, auto* q) {
+        if (!clip) copied(p, q, n);
+        else if (ratio >= (double)FLT_MIN) scaled(p, q, n, (float)ratio);
+        else scaled(p, q, n, ratio);
+    };
+    if (first < 0) chunk(static_cast<const uint16_t*>(B.in[t]) + at, static_cast<uint16_t*>(B.out[t]) + at);
+    else chunk(static_cast<const float*>(B.in[t]) + at, static_cast<float*>(B.out[t]) + at);
 }
 
 // Chunk length: TARGET_CHUNKS workgroups fill the chip several times over; below MIN_CHUNK a workgroup would not have four
