@@ -25,7 +25,6 @@ struct DenseScore {
     float out, inv_out;  // cap log2(e) and its reciprocal
     float c[8];          // odd polynomial of out * tanh
     int32_t capped, biased;
-    int32_t coarse;      // the tanh by exponential and reciprocal serves results in bf16 (or there is no cap)
 };
 
 struct DenseParams {

@@ -1,5 +1,6 @@
 // Attention among all atoms of a segment, forward: one pass over the keys with the running maximum and sum of the softmax.
 #include <initializer_list>
+#include <type_traits>
 
 #include "e2f_dense_api.h"
 
@@ -20,7 +21,8 @@ struct FwdShape {
     };
 };
 
-template <typename T, int DP, int ROWW, int KEYW>
+// COARSE: the tanh by exponential and reciprocal, for results in bf16 (see cap_scores_coarse).
+template <typename T, int DP, int ROWW, int KEYW, bool COARSE>
 __global__ __launch_bounds__(64 * ROWW * KEYW, ROWW == 1 && DP * sizeof(T) > 128 ? 1 : 2) void k_dense_fwd(DenseParams A) {
     using F = FwdShape<T, DP, ROWW, KEYW>;
     using M = typename F::M;
@@ -77,7 +79,7 @@ __global__ __launch_bounds__(64 * ROWW * KEYW, ROWW == 1 && DP * sizeof(T) > 128
         const int n = min(BN, end - t);
         for (int m = 0; m < n; m += 32) {
             f32x16 p = M::dot(tile.k, m, qf, lane);
-            if (sizeof(T) == 2 && A.score.coarse) cap_scores_coarse(p, A.score, reference_base(top));
+            if constexpr (COARSE) cap_scores_coarse(p, A.score, reference_base(top));
             else cap_scores<false>(p, p, A.score, reference_base(top));
             if (A.score.biased) bias_scores<BN>(p, x, y, z, slope, tile.place, m + 4 * half);
             if (n - m < 32) {
@@ -254,9 +256,10 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_dense_join(DenseParams A, i
 struct FwdPlan {
     int roww, keyw, parts;
     int64_t tiles;
+    bool coarse;
 };
 FwdPlan fwd_plan(const e2f_dense_args* a) {
-    FwdPlan P = {4, 1, 1, 0};
+    FwdPlan P = {4, 1, 1, 0, a->cap <= COARSE_CAP};
     const int group = a->Hq / a->Hk;
     const int64_t rows = (int64_t)a->Nq * group, S = a->S > 0 ? a->S : 1;
     if (rows <= 32 * S) {
@@ -286,9 +289,18 @@ FwdPlan fwd_plan(const e2f_dense_args* a) {
 template <typename T, int DP>
 void launch_dp(const DenseParams& A, const FwdPlan& P, hipStream_t st) {
     const dim3 grid((unsigned)(P.tiles * A.Hk), (unsigned)P.parts);
-    if (P.roww == 4) k_dense_fwd<T, DP, 4, 1><<<grid, 256, 0, st>>>(A);
-    else if (P.keyw == 4) k_dense_fwd<T, DP, 1, 4><<<grid, 256, 0, st>>>(A);
-    else k_dense_fwd<T, DP, 1, 1><<<grid, 64, 0, st>>>(A);
+    auto go = [&](auto coarse) {
+        constexpr bool COARSE = decltype(coarse)::value;
+        if (P.roww == 4) k_dense_fwd<T, DP, 4, 1, COARSE><<<grid, 256, 0, st>>>(A);
+        else if (P.keyw == 4) k_dense_fwd<T, DP, 1, 4, COARSE><<<grid, 256, 0, st>>>(A);
+        else k_dense_fwd<T, DP, 1, 1, COARSE><<<grid, 64, 0, st>>>(A);
+    };
+    if constexpr (sizeof(T) == 2) {
+        if (P.coarse) go(std::true_type{});
+        else go(std::false_type{});
+    } else {
+        go(std::false_type{});
+    }
     const int64_t rows = (int64_t)A.Nq * A.Hk * A.group;
     if (P.parts > JOIN_FEW && rows * (A.D / 4) < 65536) k_dense_join<T><<<(unsigned)rows, 64 * JOIN_WAVES, 0, st>>>(A, P.parts);
     else if (P.parts > 1) k_dense_join_few<T><<<(unsigned)((rows * (A.D / 4) + 255) / 256), 256, 0, st>>>(A, P.parts);
@@ -370,7 +382,6 @@ void dense_fill(DenseParams& A, const e2f_dense_args* a, const e2f_heads* q, con
     DenseScore& s = A.score;
     s.capped = a->cap > 0.0f;
     s.biased = a->slope != nullptr;
-    s.coarse = a->cap <= COARSE_CAP;
     s.in = s.capped ? a->scale / a->cap : (float)((double)a->scale * 1.4426950408889634);
     const double out = (double)a->cap * 1.4426950408889634;
     s.out = (float)out;
