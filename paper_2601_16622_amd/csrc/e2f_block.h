@@ -34,6 +34,10 @@ static inline e2f_status check_result_rows(const e2f_heads* x, int32_t dtype, in
     return E2F_OK;
 }
 
+// A launch has fewer than 2^32 threads along x.
+constexpr int64_t MOST_THREADS = (int64_t)1 << 32;
+static inline bool launches(int64_t blocks, int threads) { return blocks * threads < MOST_THREADS; }
+
 // Whether 4-byte elements may lie there (or nothing does).
 static inline bool word_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 static inline bool aligned_ws(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }

@@ -334,10 +334,22 @@ e2f_status e2f_qk_norm_rotate(const e2f_qk_args* a, const e2f_heads* q, const e2
     A.dy[0] = A.dy[1] = Rows{nullptr, 0, 0};
     A.out[0] = rows_of(q_out, a->dtype);
     A.out[1] = rows_of(k_out, a->dtype);
-    const Grid g = grid_of(a, INT32_MAX);
-    A.heads_per_wave = g.heads_per_wave;
-    launch<false>(a, A, g, static_cast<hipStream_t>(hip_stream));
-    E2F_HIP_CHECK(hipGetLastError());
+    // as many tokens at a time as one launch has threads for
+    const int rows = THREADS / lanes_of(a);
+    const int64_t most = (MOST_THREADS / THREADS - 1) * rows;
+    for (int64_t first = 0; first < a->N; first += most) {
+        e2f_qk_args part = *a;
+        part.N = A.N = (int32_t)(a->N - first < most ? a->N - first : most);
+        const Grid g = grid_of(&part, INT32_MAX);
+        A.heads_per_wave = g.heads_per_wave;
+        launch<false>(a, A, g, static_cast<hipStream_t>(hip_stream));
+        E2F_HIP_CHECK(hipGetLastError());
+        if (A.position) A.position += A.N;
+        for (int k = 0; k < 2; ++k) {
+            if (A.x[k].ptr) A.x[k].ptr += A.N * A.x[k].token_bytes;
+            if (A.out[k].ptr) A.out[k].ptr += A.N * A.out[k].token_bytes;
+        }
+    }
     return E2F_OK;
 }
 
