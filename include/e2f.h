@@ -426,7 +426,8 @@ typedef struct {
     int32_t dtype;          /* e2f_dtype of q, k, v, out and their gradients */
     int32_t Hq, Hk;         /* query and key heads, Hq a multiple of Hk, 1..1024 */
     int32_t D;              /* features of a head, a multiple of 8, 8..128 */
-    int32_t Nq, Nk, S;      /* query tokens, key tokens, segments; Nq Hq/Hk and Nk up to 2^31 - 1025 */
+    int32_t Nq, Nk, S;      /* query tokens, key tokens, segments; Nq Hq/Hk and Nk up to 2^31 - 1025, and no more workgroups than a launch
+                               takes (Nq Hq and Nk Hk below 2^29 with S Hk below 2^22 always pass): E2F_ERR_UNSUPPORTED otherwise */
     float scale;            /* finite */
     float cap;              /* 2^-20 .. 2^20, or 0 for none */
     const int32_t *q_offsets, *k_offsets, *q_lengths, *k_lengths;

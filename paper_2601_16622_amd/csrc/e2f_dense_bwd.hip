@@ -590,11 +590,18 @@ BwdPlan bwd_plan(const e2f_dense_args* a) {
     const int row_slots = a->D > 64 ? 256 : 512, key_slots = a->D * elem_bytes(a->dtype) > 128 ? 256 : 512;
     if (P.row_tiles) {
         const int64_t blocks = P.row_tiles * a->Hk * P.row_waves / 4 + 1, most = a->Nk / S / 256;
-        P.stat_parts = best_parts(blocks, 512, a->Nk / S * step, rows * a->Hk * 32.0 / 4.5e6, most);
-        P.row_parts = best_parts(blocks, row_slots, a->Nk / S * step, rows * a->Hk * a->D * 8.0 / 4.5e6, most);
+        P.stat_parts = best_parts(blocks, 512, a->Nk / S * step, rows * a->Hk * 32.0 / 4.5e6, rows * a->Hk, most);
+        P.row_parts = best_parts(blocks, row_slots, a->Nk / S * step, rows * a->Hk * a->D * 8.0 / 4.5e6, rows * a->Hk * (a->D / 4), most);
     }
-    if (P.key_tiles) P.key_parts = best_parts(P.key_tiles * a->Hk * P.key_waves / 4 + 1, key_slots, rows / S * step, (double)a->Nk * a->Hk * a->D * 16.0 / 4.5e6, rows / S / 256);
+    if (P.key_tiles)
+        P.key_parts = best_parts(P.key_tiles * a->Hk * P.key_waves / 4 + 1, key_slots, rows / S * step, (double)a->Nk * a->Hk * a->D * 16.0 / 4.5e6,
+                                 (int64_t)a->Nk * a->Hk * (a->D / 4), rows / S / 256);
     return P;
+}
+
+// Workgroups have up to two waves to a group of rows or keys, see launch_dp.
+bool launches(const e2f_dense_args* a, const BwdPlan& P) {
+    return e2f::launches(P.row_tiles * a->Hk, P.row_waves == 4 ? 512 : 64) && e2f::launches(P.key_tiles * a->Hk, P.key_waves == 4 ? 512 : 64);
 }
 
 template <typename T, int DP>
@@ -681,7 +688,9 @@ size_t layout(const e2f_dense_args* a, const BwdPlan& P, char* ws, DenseParams* 
 extern "C" {
 
 size_t e2f_dense_attn_backward_workspace_bytes(const e2f_dense_args* a) {
-    return dense_check_sizes(a) == E2F_OK ? layout(a, bwd_plan(a), nullptr, nullptr) : 0;
+    if (dense_check_sizes(a) != E2F_OK) return 0;
+    const BwdPlan P = bwd_plan(a);
+    return launches(a, P) ? layout(a, P, nullptr, nullptr) : 0;
 }
 
 e2f_status e2f_dense_attn_backward(const e2f_dense_args* a, const e2f_heads* q, const e2f_heads* k, const e2f_heads* v,
@@ -699,6 +708,7 @@ e2f_status e2f_dense_attn_backward(const e2f_dense_args* a, const e2f_heads* q, 
     if ((grad_slope || grad_q_pos || grad_k_pos) && !a->slope) return E2F_ERR_INVALID_ARG;
     if (!word_aligned(grad_slope) || !word_aligned(grad_q_pos) || !word_aligned(grad_k_pos)) return E2F_ERR_INVALID_ARG;
     const BwdPlan P = bwd_plan(a);
+    if (!launches(a, P)) return E2F_ERR_UNSUPPORTED;
     const size_t need = layout(a, P, nullptr, nullptr);
     if (need && (!ws || !aligned_ws(ws))) return E2F_ERR_INVALID_ARG;
     if (ws_bytes < need) return E2F_ERR_WORKSPACE_TOO_SMALL;

@@ -275,7 +275,7 @@ FwdPlan fwd_plan(const e2f_dense_args* a) {
         // 309 -> 233 with three; 100 queries over 60 000 keys on 2 key heads 291 us with eight parts,
         // 79 with 64
         const double per_key = a->dtype == E2F_BF16 ? 0.018 + 0.00027 * a->D : 0.02 + 0.001 * a->D;
-        P.parts = best_parts(blocks, 512, keys * per_key, rows * a->Hk * (a->D * 8.0) / 4.5e6, keys / 256);
+        P.parts = best_parts(blocks, 512, keys * per_key, rows * a->Hk * (a->D * 8.0) / 4.5e6, rows * a->Hk * (a->D / 4), keys / 256);
     } else {
         // a few rows: their keys over 2048 waves, each with two tiles at least
         int64_t parts = 2048 / (blocks * P.keyw);
@@ -285,6 +285,8 @@ FwdPlan fwd_plan(const e2f_dense_args* a) {
     }
     return P;
 }
+
+bool launches(const e2f_dense_args* a, const FwdPlan& P) { return e2f::launches(P.tiles * a->Hk, 64 * P.roww * P.keyw); }
 
 template <typename T, int DP>
 void launch_dp(const DenseParams& A, const FwdPlan& P, hipStream_t st) {
@@ -397,7 +399,9 @@ void dense_fill(DenseParams& A, const e2f_dense_args* a, const e2f_heads* q, con
 extern "C" {
 
 size_t e2f_dense_attn_workspace_bytes(const e2f_dense_args* a) {
-    return dense_check_sizes(a) == E2F_OK ? layout(a, fwd_plan(a), nullptr, nullptr) : 0;
+    if (dense_check_sizes(a) != E2F_OK) return 0;
+    const FwdPlan P = fwd_plan(a);
+    return launches(a, P) ? layout(a, P, nullptr, nullptr) : 0;
 }
 
 e2f_status e2f_dense_attn_forward(const e2f_dense_args* a, const e2f_heads* q, const e2f_heads* k, const e2f_heads* v,
@@ -409,6 +413,7 @@ e2f_status e2f_dense_attn_forward(const e2f_dense_args* a, const e2f_heads* q, c
         (rc = check_result_rows(out, a->dtype, a->Nq, a->Hq, a->D)) != E2F_OK)
         return rc;
     const FwdPlan P = fwd_plan(a);
+    if (!launches(a, P)) return E2F_ERR_UNSUPPORTED;
     const size_t need = layout(a, P, nullptr, nullptr);
     if (need && (!ws || !aligned_ws(ws))) return E2F_ERR_INVALID_ARG;
     if (ws_bytes < need) return E2F_ERR_WORKSPACE_TOO_SMALL;

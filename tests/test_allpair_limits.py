@@ -24,3 +24,19 @@ def test_rows_and_keys_that_a_walk_by_tiles_would_carry_past_31_bits(lib, kw):
     assert lib.e2f_dense_attn_workspace_bytes(d) == 0 and lib.e2f_dense_attn_backward_workspace_bytes(d) == 0
     assert lib.e2f_dense_attn_forward(d, h, h, h, heads(), fake, 1 << 62, None) == UNSUPPORTED
     assert lib.e2f_dense_attn_backward(d, h, h, h, h, heads(), heads(), heads(), None, None, None, fake, 1 << 62, None) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("kw", [dict(S=1 << 27, Nq=1 << 27, Nk=1 << 27), dict(S=1 << 23, Nq=1 << 30, Nk=1 << 30, Hq=2, Hk=2)])
+def test_more_workgroups_than_a_launch_takes(lib, kw):
+    """2^32 threads along a grid's first axis; 2^27 segments of a wave each are 2^33."""
+    h, d = heads(token=0), dense(**dict(dict(Hq=1, Hk=1), **kw))
+    assert lib.e2f_dense_attn_workspace_bytes(d) == 0 and lib.e2f_dense_attn_backward_workspace_bytes(d) == 0
+    assert lib.e2f_dense_attn_forward(d, h, h, h, heads(), fake, 1 << 62, None) == UNSUPPORTED
+    assert lib.e2f_dense_attn_backward(d, h, h, h, h, heads(), heads(), heads(), None, None, None, fake, 1 << 62, None) == UNSUPPORTED
+
+
+def test_sizes_that_the_header_says_pass(lib):
+    n, m = (1 << 29) - 1, (1 << 22) - 1
+    for kw in (dict(Nq=n, Nk=n, S=m), dict(Nq=n // 8, Nk=n // 8, Hq=8, Hk=8, S=m // 8, D=128), dict(Nq=n // 8, Nk=n, Hq=8, S=m), dict(Nq=m * 8, Nk=m * 65, S=m, dtype=1),
+               dict(Nq=m * 32, Nk=n, S=m), dict(Nq=n, Nk=m * 64, S=m)):
+        assert lib.e2f_dense_attn_backward_workspace_bytes(dense(**dict(dict(Hq=1, Hk=1), **kw))) > 0
