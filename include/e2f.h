@@ -367,8 +367,8 @@ typedef struct {
  *   y   = u with the first rotary_dim features turned pairwise: for pair i of rotary_dim/2, features a and b,
  *         y_a = u_a cos f - u_b sin f,  y_b = u_b cos f + u_a sin f,  f = position[t] position_scale theta^(-2i/rotary_dim)
  *         HALF: (a, b) = (i, i + rotary_dim/2);  INTERLEAVED: (2i, 2i + 1)
- * Angles are formed in 64 bits and reduced to one turn before they are rounded; everything else is binary32, rounded
- * once to the feature type.  q and q_out (k and k_out) may be the same rows; other overlaps are not allowed.
+ * Angles are formed in 64 bits and reduced to one turn before they are rounded; everything else is binary32 (cosines and sines with bf16
+ * features off by 2^-22 at most, in the gradients of the weights too), rounded once to the feature type.  q and q_out (k and k_out) may be the same rows; other overlaps are not allowed.
  * Hq or Hk may be 0 (its e2f_heads is then ignored and may be NULL), for queries and keys of different tokens.
  */
 typedef enum { E2F_ROTARY_HALF = 0, E2F_ROTARY_INTERLEAVED = 1 } e2f_rotary_layout;

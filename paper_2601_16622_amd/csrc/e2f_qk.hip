@@ -30,7 +30,8 @@ struct QkParams {
 enum Partner { IN_LANE, OTHER_LANE, FROM_MEMORY };
 
 // cos and signed sin of a lane's features: y_e = c_e u_e + s_e u_partner(e).  For bf16 by the instructions for turns, whose absolute
-// error of about 2^-21 is far below a result's rounding, 2^-9; with the library's functions the angles were 40 % of the instructions.
+// error (1.25e-7 = 2^-22.9 at most over 4 M angles of a turn, 3.4e-8 in the mean) is far below a result's rounding, 2^-8, and about one of binary32
+// in the gradients of the weights; with the library's functions the angles were 40 % of the instructions (backward pass of 10 000 tokens 4 % slower).
 template <typename T, int V, Partner P>
 __device__ __forceinline__ void angles(const QkParams& A, int e0, int position, float (&c)[V], float (&s)[V]) {
     const int half = A.rot >> 1;
