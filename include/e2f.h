@@ -368,7 +368,8 @@ typedef struct {
  *         y_a = u_a cos f - u_b sin f,  y_b = u_b cos f + u_a sin f,  f = position[t] position_scale theta^(-2i/rotary_dim)
  *         HALF: (a, b) = (i, i + rotary_dim/2);  INTERLEAVED: (2i, 2i + 1)
  * Angles are formed in 64 bits and reduced to one turn before they are rounded; everything else is binary32 (cosines and sines with bf16
- * features off by 2^-22 at most, in the gradients of the weights too), rounded once to the feature type.  q and q_out (k and k_out) may be the same rows; other overlaps are not allowed.
+ * features off by 2^-22 at most, in the gradients of the weights too), rounded once to the feature type.  (A row whose squares sum up beyond binary32,
+ * features of 1e19 / D^(1/2), has r = 0 and comes out as zeros.)  q and q_out (k and k_out) may be the same rows; other overlaps are not allowed.
  * Hq or Hk may be 0 (its e2f_heads is then ignored and may be NULL), for queries and keys of different tokens.
  */
 typedef enum { E2F_ROTARY_HALF = 0, E2F_ROTARY_INTERLEAVED = 1 } e2f_rotary_layout;
@@ -415,7 +416,8 @@ e2f_status e2f_qk_norm_rotate_backward(const e2f_qk_args *a, const e2f_heads *q,
  *   q_pos, k_pos, slope   device float [Nq][3], [Nk][3], [Hq]; all three or none.  A coordinate beyond 5e18 in size, infinity too, counts as 5e18
  * Keys outside their segment's length and queries outside any segment's are not read.  A query without keys gets a zero row;
  * rows of out and of the gradients that no segment's length covers are left as they were.  No result may overlap an operand or
- * another result.  A row's result is the same bits whatever the rows beside it hold.
+ * another result.  A row's result is the same bits whatever the rows beside it hold.  Operands are finite: an infinite entry may come out
+ * as NaN in what it enters by the formulas, and in nothing else.
  * A score s is off by 2^-22 of its size or so, and a weight with it: a query that is 2^20 / slope or farther from its nearest key has no
  * meaningful weights, and what it brings to gradients may be NaN.
  * Scores, softmax statistics and sums are binary32; with bf16 features the weights and factors that meet the matrix cores are the sum of two

@@ -128,3 +128,27 @@ def test_a_query_far_away_reaches_no_other_row(dtype):
     x["q_pos"][11, 0] = float("nan")
     got = call(x, 20.0, backward=False)["out"]
     assert bool(torch.isnan(got[11]).all()) and torch.equal(got[12:], want["out"][12:])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [32, 64, 96])
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+def test_entries_that_are_not_finite_stay_in_what_they_enter(dtype, D, bad):
+    x = make(dtype, D, 2, 1, [60, 70], [80, 50], True, 35)
+    want = call(x, 20.0)
+    segment = {n: 60 if n in ("out", "q", "q_pos") else 80 for n in want if n != "slope"}
+    y = dict(x, q=x["q"].clone())
+    y["q"][7, 1, 3] = bad
+    got = call(y, 20.0)
+    for n in ("out", "q"):
+        assert torch.equal(got[n][:, 0], want[n][:, 0]) and torch.equal(got[n][:7], want[n][:7]) and torch.equal(got[n][8:], want[n][8:]), n
+    assert all(torch.equal(got[n][b:], want[n][b:]) for n, b in segment.items())
+    for name, at in (("k", 80 + 3), ("v", 80 + 3), ("go", 60 + 3)):
+        y = dict(x, **{name: x[name].clone()})
+        y[name][at, 0, 5] = bad
+        got = call(y, 20.0)
+        assert all(torch.equal(got[n][:b], want[n][:b]) for n, b in segment.items()), name
+        if name == "go":
+            assert torch.equal(got["out"], want["out"])
+        if name == "v":
+            assert not bool(torch.isfinite(got["out"][60:, :, 5]).any())
