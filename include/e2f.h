@@ -420,9 +420,11 @@ e2f_status e2f_qk_norm_rotate_backward(const e2f_qk_args *a, const e2f_heads *q,
  * as NaN in what it enters by the formulas, and in nothing else.
  * A score s is off by 2^-22 of its size or so, and a weight with it: a query that is 2^20 / slope or farther from its nearest key has no
  * meaningful weights, and what it brings to gradients may be NaN.
- * Scores, softmax statistics and sums are binary32; with bf16 features the weights and factors that meet the matrix cores are the sum of two
- * bf16 each, off by 2^-15 at most, and the forward pass's scores under a cap of up to 128 are off by 2^-22 of the cap at most.  The gradients of
- * slope and places take no such rounding.
+ * Scores, softmax statistics and sums are binary32.  With fp32 features up to D = 64 a product leaves out up to 2^-21 of its size, 2^-24 in the
+ * mean.  With bf16 features the weights and factors that meet the matrix cores are the sum of two bf16 each, off by 2^-15 at most, and the
+ * forward pass's scores under a cap of up to 128 are off by 2^-22 of the cap at most.  The gradients of slope and places take no such rounding.
+ * Work is shared out by the mean length of the segments, since the host does not see the offsets: one long segment among many short or
+ * empty ones runs on few workgroups and is better a call of its own.
  */
 typedef struct {
     int32_t dtype;          /* e2f_dtype of q, k, v, out and their gradients */
