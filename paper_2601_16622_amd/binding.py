@@ -440,6 +440,8 @@ def _qk_args(where, q, k, position=None, weight_q=None, weight_k=None, rotary_di
     N, _, D = x.shape
     if N > _INT32_MAX:
         _refuse(where)
+    if k is not None and k.dim() != 3:
+        _refuse(f"{where}: k")
     Hq, Hk = 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
     a = QkArgs(kind, N, Hq, Hk, D, rotary_dim, ROTARY.get(layout, layout), eps, theta, position_scale,
                None if position is None else _plain(position, torch.int32, device, (N,), where, "position"),

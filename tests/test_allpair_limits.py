@@ -2,6 +2,7 @@
 import os
 
 import pytest
+import torch
 
 from paper_2601_16622_amd import binding as B
 from test_allpair_host import UNSUPPORTED, dense, fake, heads
@@ -40,3 +41,13 @@ def test_sizes_that_the_header_says_pass(lib):
     for kw in (dict(Nq=n, Nk=n, S=m), dict(Nq=n // 8, Nk=n // 8, Hq=8, Hk=8, S=m // 8, D=128), dict(Nq=n // 8, Nk=n, Hq=8, S=m), dict(Nq=m * 8, Nk=m * 65, S=m, dtype=1),
                dict(Nq=m * 32, Nk=n, S=m), dict(Nq=n, Nk=m * 64, S=m)):
         assert lib.e2f_dense_attn_backward_workspace_bytes(dense(**dict(dict(Hq=1, Hk=1), **kw))) > 0
+
+
+@pytest.mark.parametrize("k", [torch.zeros(16), torch.zeros(4, 16), torch.zeros(())])
+def test_binding_refuses_keys_of_another_rank(lib, k):
+    q = torch.zeros(4, 2, 16)
+    for call in (lambda: B.e2f_qk_norm_rotate(q, k, q, k), lambda: B.e2f_qk_norm_rotate_backward(q, k, q, k, q, k, None, None, None),
+                 lambda: B.e2f_qk_norm_rotate_backward_workspace_bytes(q, k), lambda: B.e2f_dense_attn_workspace_bytes(q, k, 1)):
+        with pytest.raises(B.E2fError) as e:
+            call()
+        assert e.value.code == B.E2F_ERR_INVALID_ARG
