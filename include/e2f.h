@@ -381,7 +381,7 @@ typedef struct {
     int32_t layout;         /* e2f_rotary_layout */
     float eps;              /* > 0 */
     double theta;           /* > 0 */
-    double position_scale;  /* finite; below 1 it compresses the positions of chains longer than a model was trained on */
+    double position_scale;  /* finite, as are the angles at positions of up to 2^31; below 1 it compresses the positions of chains longer than a model was trained on */
     const int32_t *position;                  /* device [N]; may be NULL if rotary_dim is 0 */
     const float *weight_q, *weight_k;         /* device [D]; NULL: ones */
 } e2f_qk_args;

@@ -229,6 +229,9 @@ e2f_status check(const e2f_qk_args* a) {
     if (a->layout != E2F_ROTARY_HALF && a->layout != E2F_ROTARY_INTERLEAVED) return E2F_ERR_INVALID_ARG;
     if (!(a->eps > 0.0f) || !isfinite(a->eps) || !(a->theta > 0.0) || !isfinite(a->theta) || !isfinite(a->position_scale))
         return E2F_ERR_INVALID_ARG;
+    // every pair's angle at a position of up to 2^31 has to be a binary64 number; the rates are 1 and, at the last pair, theta^(2/rotary_dim - 1)
+    const double rate = a->rotary_dim ? fmax(1.0, pow(a->theta, 2.0 / a->rotary_dim - 1.0)) : 1.0;
+    if (!isfinite(fabs(a->position_scale) * rate * 0x1p31)) return E2F_ERR_INVALID_ARG;
     if (a->D % 8 || a->D > MAX_D || a->Hq > 1024 || a->Hk > 1024) return E2F_ERR_UNSUPPORTED;
     if (a->N > 0 && a->rotary_dim > 0 && !a->position) return E2F_ERR_INVALID_ARG;
     if (!word_aligned(a->position) || !word_aligned(a->weight_q) || !word_aligned(a->weight_k)) return E2F_ERR_INVALID_ARG;

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2601_16622_amd import binding as B
-from test_allpair_host import UNSUPPORTED, dense, fake, heads
+from test_allpair_host import INVALID, UNSUPPORTED, dense, fake, heads, qk
 
 MOST = 2 ** 31 - 1
 
@@ -51,3 +51,17 @@ def test_binding_refuses_keys_of_another_rank(lib, k):
         with pytest.raises(B.E2fError) as e:
             call()
         assert e.value.code == B.E2F_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("kw", [dict(position_scale=1e300), dict(position_scale=-1e299), dict(theta=1e-300, rotary_dim=16, position_scale=1e100), dict(theta=5e-324, rotary_dim=16, position_scale=1e50)])
+def test_angles_beyond_binary64(lib, kw):
+    """Infinite angles made every rotated feature a NaN."""
+    h = heads()
+    assert lib.e2f_qk_norm_rotate_backward_workspace_bytes(qk(**kw)) == 0
+    assert lib.e2f_qk_norm_rotate_backward(qk(**kw), h, h, h, h, h, h, None, None, fake, 1 << 30, None) == INVALID
+    assert lib.e2f_qk_norm_rotate(qk(**kw), h, h, h, h, None) == INVALID
+
+
+@pytest.mark.parametrize("kw", [dict(theta=0.5), dict(theta=1e300), dict(position_scale=1e200, rotary_dim=0), dict(theta=1e-3, rotary_dim=2)])
+def test_angles_within_binary64(lib, kw):
+    assert lib.e2f_qk_norm_rotate_backward_workspace_bytes(qk(**kw)) > 0
