@@ -182,9 +182,12 @@ __global__ __launch_bounds__(256) void k_dense_join_few(DenseParams A, int parts
     else *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
 }
 
-// For many parts of rows that do not fill the chip so, a workgroup for a row; its waves share the parts, a lane forms a part's factor, then all lanes walk over the features of the wave's parts, whose loads do
-// not wait for each other.
-constexpr int JOIN_WAVES = 16, JOIN_FEW = 8;
+// For more than JOIN_FEW parts of fewer than JOIN_ROWS rows, which do not fill the chip so, a workgroup for a row; its waves share the parts, a lane
+// forms a part's factor, then all lanes walk over the features of the wave's parts, whose loads do not wait for each other.  Both ways, by rows
+// and by threads: 8 rows of 64 features over 1 600 keys (6 parts) 14.2 and 13.3 us, 2 100 keys (8 parts) 14.0 and 14.3, 4 500 keys 14.4 and
+// 18.3; over 60 000 keys 1 280 rows of 64 features 119 and 121, 1 600 rows 139 and 133 (of 32 or 128 features: 1 024 rows 91 and 103, 117
+// and 129, 1 600 rows 128 and 122, 163 and 157), 2 400 rows 195 and 165.
+constexpr int JOIN_WAVES = 16, JOIN_FEW = 8, JOIN_ROWS = 1400;
 template <typename T>
 __global__ __launch_bounds__(64 * JOIN_WAVES) void k_dense_join(DenseParams A, int parts) {
     __shared__ float sums[JOIN_WAVES][128], weight[JOIN_WAVES], best[JOIN_WAVES];
@@ -272,8 +275,7 @@ FwdPlan fwd_plan(const e2f_dense_args* a) {
     if (P.roww == 4) {
         // two workgroups to a compute unit; a round over 10 000 keys with 64 (128) features takes 354 (524) us in bf16, 800 (1 500) in
         // fp32.  Parts instead of one: 10 000 atoms, 8 heads, 632 workgroups 708 -> 569 us with two; 4 000 atoms in fp32, 264 workgroups,
-        // 309 -> 233 with three; 100 queries over 60 000 keys on 2 key heads 291 us with eight parts,
-        // 79 with 64
+        // 309 -> 233 with three; 40 (100) queries over 60 000 keys on 2 key heads 317 (315) us with eight parts, 58 (86) with up to 64
         const double per_key = a->dtype == E2F_BF16 ? 0.018 + 0.00027 * a->D : 0.02 + 0.001 * a->D;
         P.parts = best_parts(blocks, 512, keys * per_key, rows * a->Hk * (a->D * 8.0) / 4.5e6, rows * a->Hk * (a->D / 4), keys / 256);
     } else {
@@ -304,7 +306,7 @@ void launch_dp(const DenseParams& A, const FwdPlan& P, hipStream_t st) {
         go(std::false_type{});
     }
     const int64_t rows = (int64_t)A.Nq * A.Hk * A.group;
-    if (P.parts > JOIN_FEW && rows * (A.D / 4) < 65536) k_dense_join<T><<<(unsigned)rows, 64 * JOIN_WAVES, 0, st>>>(A, P.parts);
+    if (P.parts > JOIN_FEW && rows < JOIN_ROWS) k_dense_join<T><<<(unsigned)rows, 64 * JOIN_WAVES, 0, st>>>(A, P.parts);
     else if (P.parts > 1) k_dense_join_few<T><<<(unsigned)((rows * (A.D / 4) + 255) / 256), 256, 0, st>>>(A, P.parts);
 }
 
