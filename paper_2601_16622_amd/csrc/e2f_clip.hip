@@ -3,8 +3,9 @@
 //
 // The tensors are cut into chunks of one length, a workgroup each, so that a few large and many tiny tensors load the
 // chip alike.  A chunk's sum of squares is a binary64 partial sum in the workspace; the scaling kernel's workgroups each
-// sum all of these (a few thousand, out of the L2) in the same order, which saves the launch and the wait of a
-// reduction of its own and gives every workgroup the same factor.  Tensors travel in the kernel's arguments, TENSORS of
+// sum all of these (out of the L2) in the same order, which saves the launch and the wait of a reduction of its own and gives every workgroup
+// the same factor.  They are about 2 000, and one for each tensor at least: with thousands of small tensors every workgroup sums thousands
+// (1 000 tensors of 2 000 elements take 79 us, 3 000 277 us, 10 000 1 315 us).  Tensors travel in the kernel's arguments, TENSORS of
 // them a launch, so that a captured graph needs no table in device memory.
 #include <float.h>
 

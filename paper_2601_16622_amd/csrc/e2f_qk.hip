@@ -260,8 +260,10 @@ void fill(QkParams& A, const e2f_qk_args* a) {
 }
 
 // Grid along the tokens and the heads.  Heads of a token share its angles, so a wave takes all of them where the tokens alone make
-// enough workgroups, and fewer heads where they do not.  For 640 workgroups or more: at 10 000 tokens, 16 heads of 64 bf16
-// features (313 workgroups along the tokens), forward and backward take 48.9 us with one share of the heads, 37.3 with two, 35.0 with three, 39.7 with four.
+// enough workgroups, and fewer heads where they do not.  For 640 workgroups or more, from both sides (a training step, 16 heads, with
+// 320 / 640 / 1 280 workgroups): 3 000 tokens of 64 bf16 features 22.9 / 22.4 / 22.0 us, 10 000 37.6 / 36.6 / 41.3, 30 000 77.2 / 77.3 / 88.1; in
+// fp32 30.6 / 24.1 / 25.8, 63.4 / 54.1 / 58.2, 138 / 139 / 146; 10 000 tokens of 16 bf16 features 21.9 / 22.5 / 31.0, 3 000 of 128 37.5 / 34.1 /
+// 41.5.  One share of the heads takes 37 us for 300 tokens in place of 12.
 struct Grid {
     unsigned x, y;
     int heads_per_wave;
