@@ -586,8 +586,8 @@ BwdPlan bwd_plan(const e2f_dense_args* a) {
     P.row_tiles = a->Nq ? dense_tiles(a->Nq, group, a->S, 32 * P.row_waves) : 0;
     P.key_tiles = a->Nk ? dense_tiles(a->Nk, 1, a->S, 32 * P.key_waves) : 0;
     // times of a round for a step along the other side, and of a part's sums, written and read at 4.5 TB/s.  At 5 003 keys of 2 heads and
-    // 128 features, 314 workgroups over rows take 475 us in one part, 401 in three and 387 in four; 80 over keys, 20 012 rows, take
-    // 1 600 us in one part and 533 in twelve as in three
+    // 128 bf16 features, 314 workgroups over rows take 589 us in one part, 466 in three and 456 in four; 80 over keys, 20 012 rows, take
+    // 1 605 us in one part, 646 in three, 638 in four and 649 in thirteen
     const double step = a->dtype == E2F_BF16 ? 0.03 + 0.0004 * a->D : 0.05 + 0.004 * a->D;
     const int row_slots = a->D > 64 ? 256 : 512, key_slots = a->D * elem_bytes(a->dtype) > 128 ? 256 : 512;
     if (P.row_tiles) {

@@ -273,10 +273,11 @@ FwdPlan fwd_plan(const e2f_dense_args* a) {
     if (P.tiles == 0) return P;
     const int64_t blocks = P.tiles * a->Hk, keys = a->Nk / S;
     if (P.roww == 4) {
-        // two workgroups to a compute unit; a round over 10 000 keys with 64 (128) features takes 354 (524) us in bf16, 800 (1 500) in
-        // fp32.  Parts instead of one: 10 000 atoms, 8 heads, 632 workgroups 708 -> 569 us with two; 4 000 atoms in fp32, 264 workgroups,
-        // 309 -> 233 with three; 40 (100) queries over 60 000 keys on 2 key heads 317 (315) us with eight parts, 58 (86) with up to 64
-        const double per_key = a->dtype == E2F_BF16 ? 0.018 + 0.00027 * a->D : 0.02 + 0.001 * a->D;
+        // two workgroups to a compute unit; a round over 10 000 keys with 64 (128) features takes 390 (590) us in bf16, 800 (1 500) in
+        // fp32.  Parts instead of one: 10 000 atoms, 8 heads, 632 workgroups 776 -> 654 us with two (687 with three); 4 000 atoms in fp32,
+        // 264 workgroups, 304 -> 243 with three; 40 (100) queries over 60 000 keys on 2 key heads 317 (315) us with eight parts, 58 (86)
+        // with up to 64
+        const double per_key = a->dtype == E2F_BF16 ? 0.02 + 0.0003 * a->D : 0.02 + 0.001 * a->D;
         P.parts = best_parts(blocks, 512, keys * per_key, rows * a->Hk * (a->D * 8.0) / 4.5e6, rows * a->Hk * (a->D / 4), keys / 256);
     } else {
         // a few rows: their keys over 2048 waves, each with two tiles at least
